@@ -54,10 +54,14 @@ typedef enum la_status {
     LA_ERR_EMPTY_SUFFIX = 3,      /* resume with B_i == N_i (nothing to schedule)       */
     LA_ERR_MISALIGNED_STATE = 4,  /* resume with B_i not a multiple of C                */
     LA_ERR_HIP = 5,               /* HIP runtime reported an error                      */
-    LA_ERR_WORKSPACE = 6          /* workspace smaller than la_prefill_workspace_bytes  */
+    LA_ERR_WORKSPACE = 6          /* workspace smaller than the call's *_workspace_bytes */
 } la_status;
 
-typedef enum la_dtype { LA_F32 = 0, LA_BF16 = 1 } la_dtype;
+typedef enum la_dtype {
+    LA_F32 = 0,
+    LA_BF16 = 1,
+    LA_FP8_E4M3 = 2               /* attention caches only                          */
+} la_dtype;
 
 typedef enum la_variant {
     LA_GDR_LITERAL = 0,           /* prediction S_{t-1}^T k_t                 */
@@ -418,6 +422,184 @@ la_status la_state_save_host(const float *states, int64_t n_items, int64_t page_
 la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const int32_t *page_ids_dev,
                                 float *states, int64_t n_items, int64_t page_elems,
                                 int32_t *err_count_dev, void *stream, void *done_event);
+
+/* ------------------------------------------------------------------------
+ * The attention side of a hybrid cache: the attention layers of the model
+ * whose linear-attention layers the calls above run (section 2.1: attention
+ * entries and checkpointed state move together).  A sequence's keys and
+ * values lie in blocks of the engine's cache, the blocks that
+ * la_hybrid_restore brings back; la_kv_write fills them, la_attn_prefill_paged
+ * and la_attn_decode read them, and la_blocks_* keep their book.
+ *
+ * Attention, for every token and query head h (its key head: h / G, with
+ * G = q_heads / kv_heads), over the visible keys j:
+ *
+ *   s_j = scale <q, k_j>,  p_j = exp(s_j - max s),  o = sum p_j v_j / sum p_j
+ *
+ * Key j of a sequence is visible to its token at position x when j <= x and
+ * j < kv_len; the last token of a call is at position kv_len - 1.  A token that
+ * sees no key (or whose every score is -inf) has o = 0; keys and values that
+ * it does not see have no effect on it, infinities and NaN included (one
+ * exception: an infinite value with a weight that rounds to zero gives
+ * infinity or NaN).  Scores, maxima and sums are fp32; with bf16 inputs the
+ * weights p_j are rounded to bf16 for the product with v.  Results do not
+ * depend on the other sequences of a call: how a row's keys are cut into
+ * tiles and parts follows from its own sequence (and group) alone.
+ * --------------------------------------------------------------------- */
+
+/* Shape of an attention call.  Strides are elements from one token to the
+ * next, so that q, k and v may be slices of one projection's output; 0 stands
+ * for packed rows.  Heads of a token are packed.  Rows lie on 16-byte lines. */
+typedef struct la_attn_shape {
+    int32_t n_seqs;                  /* >= 1                                       */
+    int32_t q_heads, kv_heads;       /* q_heads a multiple of kv_heads             */
+    int32_t head_dim;                /* built: 64, 128                             */
+    int32_t io_dtype;                /* LA_BF16 or LA_F32: q, k, v, o              */
+    float scale;                     /* > 0                                        */
+    int64_t q_stride, k_stride, v_stride, o_stride;
+} la_attn_shape;
+
+/* One attention layer's keys and values in the cache.  Block b begins at cache
+ * + b * block_bytes; at k_offset in it lie this layer's keys, at v_offset its
+ * values, each [kv_heads, block_tokens, head_dim]; other layers share the
+ * block.  Token x of sequence i is in slot x mod block_tokens of block
+ * block_table[i][x / block_tokens].  An entry outside [0, n_blocks) where a
+ * key is visible or written counts in err_count (at least once; device
+ * int32, may be NULL), reads as zero keys and values and is not written. */
+typedef struct la_kv_layer {
+    void *cache;                     /* device [n_blocks, block_bytes], 16-byte aligned */
+    int64_t n_blocks, block_bytes;   /* block_bytes a multiple of 16               */
+    int64_t k_offset, v_offset;      /* multiples of 16                            */
+    int32_t block_tokens;            /* a power of two, 16 to 256                  */
+    int32_t kv_heads, head_dim;
+    int32_t dtype;                   /* LA_BF16 or LA_FP8_E4M3 (bf16 calls), LA_F32 (fp32 calls) */
+    float k_scale, v_scale;          /* 8-bit: what a stored 1 stands for; else 1  */
+    const int32_t *block_table;      /* device [n_seqs, max_blocks]                */
+    int64_t max_blocks;
+    int32_t *err_count;
+} la_kv_layer;
+
+/*
+ * la_attn_prefill - causal attention of whole prompts over packed keys and
+ * values: q, o [T, q_heads, head_dim], k, v [T, kv_heads, head_dim] in
+ * io_dtype, sequence i at rows cu_seqlens[i] .. cu_seqlens[i+1]-1 (empty
+ * sequences allowed).  cu_seqlens_dev/host as for la_prefill.  workspace:
+ * la_attn_prefill_workspace_bytes(shape, cu_seqlens_host, NULL) bytes.
+ */
+la_status la_attn_prefill(const la_attn_shape *shape, const void *q, const void *k, const void *v,
+                          const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, void *o,
+                          void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * la_attn_prefill_paged - the same for tokens whose keys and values (their
+ * own, and those of the prefix before them) are in the cache: the suffix
+ * [B, N) of a resumed prompt after la_hybrid_restore and la_kv_write, or a
+ * whole prompt.  kv_len_dev/host int32 [n_seqs]: N_i, keys of sequence i;
+ * its tokens are the last cu[i+1] - cu[i] of them.  k_stride and v_stride are
+ * not used.  workspace: la_attn_prefill_workspace_bytes(shape,
+ * cu_seqlens_host, kv_len_host) bytes.
+ */
+la_status la_attn_prefill_paged(const la_attn_shape *shape, const la_kv_layer *layer, const void *q,
+                                const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host,
+                                const int32_t *kv_len_dev, const int32_t *kv_len_host, void *o,
+                                void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace of the two calls above; 0 for invalid arguments.  Host only. */
+size_t la_attn_prefill_workspace_bytes(const la_attn_shape *shape, const int32_t *cu_seqlens_host,
+                                       const int32_t *kv_len_host);
+
+/* Groups of consecutive sequences whose block tables begin with the same
+ * blocks.  Group g is sequences cu_group[g] .. cu_group[g+1]-1 (non-decreasing,
+ * within [0, n_seqs]; sequences outside every group share nothing); its first
+ * prefix_len[g] keys are read once for all of it, through the table of its
+ * first sequence.  Any length serves, whole blocks or not. */
+typedef struct la_prefix_groups {
+    int32_t n_groups;
+    int32_t max_group;               /* sequences of the largest group              */
+    const int32_t *cu_group_dev;     /* device [n_groups + 1]                       */
+    const int32_t *prefix_len_dev;   /* device [n_groups]                           */
+    int64_t max_prefix_len;          /* at least every prefix_len                   */
+} la_prefix_groups;
+
+/*
+ * la_attn_decode - attention of one new token per sequence (section 5's
+ * continuations): q, o [n_seqs, q_heads, head_dim]; kv_len_dev int32
+ * [n_seqs]: keys of each sequence, its new token's included (0: o = 0).
+ * Lengths, tables and groups are read on the device only, so that a captured
+ * call can be replayed after they change, up to max_kv_len (a longer kv_len is
+ * cut there and counts in err_count) and max_prefix_len.  groups: NULL when
+ * nothing is shared.  workspace: la_attn_decode_workspace_bytes(shape,
+ * max_kv_len, max_prefix_len) bytes; nothing in it has to start at zero.
+ */
+la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, const void *q,
+                         const int32_t *kv_len_dev, int64_t max_kv_len, const la_prefix_groups *groups,
+                         void *o, void *workspace, size_t ws_bytes, void *stream);
+size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv_len, int64_t max_prefix_len);
+
+/*
+ * la_kv_write - new keys and values into the cache: k, v [n_tokens, kv_heads,
+ * head_dim] in io_dtype (token strides as in la_attn_shape), sequence i at
+ * rows cu_seqlens[i] .. cu_seqlens[i+1]-1; its tokens become keys kv_len[i] -
+ * (cu[i+1] - cu[i]) .. kv_len[i] - 1.  An 8-bit cache holds x / scale rounded
+ * to nearest even, values beyond +-448 at +-448, NaN as NaN.  A position
+ * below zero or past the table counts in err_count and is not written.
+ */
+la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const int32_t *cu_seqlens_dev, int32_t n_seqs,
+                      int64_t n_tokens, const int32_t *kv_len_dev, void *stream);
+
+/* The blocks of a cache and their book, all on the device.  table: one row
+ * per request, -1 where there is no block; ref_count[b]: entries that name
+ * block b (0: free); free_list[0 .. *free_count - 1]: the free ids, taken
+ * from the end.  Blocks are opaque bytes: KV blocks of all layers, or state
+ * pages.  Calls that take or return several blocks do so in a fixed order,
+ * so the same calls give the same ids.  err_count (may be NULL) counts row and
+ * block ids out of range, lengths past the table, blocks that were missing and
+ * references that were taken back twice; the call does the rest of its work. */
+typedef struct la_block_pool {
+    void *cache;                     /* [n_blocks, block_bytes], 16-byte aligned    */
+    int64_t n_blocks, block_bytes;
+    int64_t n_rows, max_blocks;
+    int32_t block_tokens;            /* a power of two                              */
+    int32_t *table;                  /* [n_rows, max_blocks]                        */
+    int32_t *ref_count;              /* [n_blocks]                                  */
+    int32_t *free_list;              /* [n_blocks]                                  */
+    int32_t *free_count;             /* [1]                                         */
+    int32_t *err_count;
+} la_block_pool;
+
+/* la_blocks_copy - block dst_ids[i] = block src_ids[i] for every i; either id
+ * -1 skips the pair.  No destination may be named twice or be a source.  Uses
+ * the pool's cache, n_blocks, block_bytes and err_count only. */
+la_status la_blocks_copy(const la_block_pool *pool, const int32_t *src_ids_dev, const int32_t *dst_ids_dev,
+                         int64_t n, void *stream);
+
+/* la_blocks_fork - row child_rows[i] becomes a continuation of the first
+ * len[i] tokens of row parent_rows[i]: it shares the whole blocks, and a
+ * last block inside which the tokens end is copied into a fresh one, so that
+ * parent and child can both go on.  What the child's row held before is
+ * overwritten.  Children are distinct and no parents of the same call; at
+ * most 65,535 forks.  A fork that finds no free block gets -1 there. */
+la_status la_blocks_fork(const la_block_pool *pool, const int32_t *parent_rows_dev, const int32_t *child_rows_dev,
+                         const int32_t *len_dev, int64_t n, void *stream);
+
+/* la_blocks_extend - every missing entry of row rows[i] below
+ * ceil(len[i] / block_tokens) gets a fresh block.  Rows are distinct. */
+la_status la_blocks_extend(const la_block_pool *pool, const int32_t *rows_dev, const int32_t *len_dev,
+                           int64_t n, void *stream);
+
+/* la_blocks_free - empties rows; blocks that no entry names any more go on
+ * the free list, ids ascending. */
+la_status la_blocks_free(const la_block_pool *pool, const int32_t *rows_dev, int64_t n, void *stream);
+
+/* la_blocks_compact - moves the L live blocks into ids 0 .. L-1: the k-th live
+ * id at or past L goes to the k-th free id below L.  Table, counts and free
+ * list follow (the lowest free id on top).  new_ids_dev ([n_blocks], may be
+ * NULL) receives every block's new id, -1 for free ones, for tables kept
+ * elsewhere. */
+la_status la_blocks_compact(const la_block_pool *pool, int32_t *new_ids_dev, void *workspace, size_t ws_bytes,
+                            void *stream);
+size_t la_blocks_compact_workspace_bytes(int64_t n_blocks);
 
 /* Name of a status code (static string). */
 const char *la_status_string(la_status status);

@@ -147,3 +147,104 @@ def prefill_resume(x: DeviceInputs, starts: Sequence[int], state_in: torch.Tenso
                    variant: int = la.LA_GDR_LITERAL, scale: float = 1.0,
                    emit_ckpt: bool = True) -> PrefillResult:
     return Prefill(x, interval, variant, scale, starts, emit_ckpt).run(state_in)
+
+
+# ---------------------------------------------------------------------------
+# the attention side of a hybrid cache
+# ---------------------------------------------------------------------------
+
+class AttnPrefill:
+    """Causal attention of prompts: lengths, workspace and output of one batch.
+
+    new: tokens of each sequence in the call; kv: keys of each sequence, for
+    calls over a cache (run_paged; None: as many as its tokens)."""
+
+    def __init__(self, q_heads: int, kv_heads: int, head_dim: int, new: Sequence[int],
+                 kv: Optional[Sequence[int]] = None, dtype=torch.bfloat16, scale: Optional[float] = None,
+                 device="cuda"):
+        self.shape = la.make_attn_shape(len(new), q_heads, kv_heads, head_dim, la._dtype_of(dtype), scale)
+        self.cu_host = np.concatenate([[0], np.cumsum(np.asarray(new, np.int64))]).astype(np.int32)
+        self.kv_host = None if kv is None else np.ascontiguousarray(kv, dtype=np.int32)
+        self.cu_dev = torch.from_numpy(self.cu_host).to(device)
+        self.kv_dev = None if kv is None else torch.from_numpy(self.kv_host).to(device)
+        self.o = torch.empty((int(self.cu_host[-1]), q_heads, head_dim), dtype=dtype, device=device)
+        n = la.la_attn_prefill_workspace_bytes(self.shape, self.cu_host, self.kv_host)
+        if n == 0:
+            raise ValueError(la.last_error_message())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+
+    def run(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> torch.Tensor:
+        la.la_attn_prefill(self.shape, q, k, v, self.cu_dev, self.cu_host, self.o, self.workspace, stream)
+        return self.o
+
+    def run_paged(self, layer: la.LaKvLayer, q: torch.Tensor, stream=None) -> torch.Tensor:
+        la.la_attn_prefill_paged(self.shape, layer, q, self.cu_dev, self.cu_host, self.kv_dev, self.kv_host, self.o,
+                                 self.workspace, stream)
+        return self.o
+
+
+class AttnDecode:
+    """Attention of one new token per sequence, up to max_kv_len keys each.
+
+    cu_group: device int32 [n_groups + 1], the groups of consecutive sequences
+    that share a prefix of at most max_prefix_len keys (None: nothing shared);
+    max_group: the most sequences of a group (None: read from cu_group)."""
+
+    def __init__(self, n_seqs: int, q_heads: int, kv_heads: int, head_dim: int, max_kv_len: int,
+                 dtype=torch.bfloat16, scale: Optional[float] = None, cu_group: Optional[torch.Tensor] = None,
+                 max_prefix_len: int = 0, max_group: Optional[int] = None, device="cuda"):
+        self.shape = la.make_attn_shape(n_seqs, q_heads, kv_heads, head_dim, la._dtype_of(dtype), scale)
+        self.max_kv_len, self.cu_group, self.max_prefix_len = int(max_kv_len), cu_group, int(max_prefix_len)
+        if cu_group is not None and max_group is None:
+            max_group = int((cu_group[1:] - cu_group[:-1]).max()) if cu_group.numel() > 1 else 0
+        self.max_group = max_group
+        self.o = torch.empty((n_seqs, q_heads, head_dim), dtype=dtype, device=device)
+        n = la.la_attn_decode_workspace_bytes(self.shape, self.max_kv_len, self.max_prefix_len)
+        if n == 0:
+            raise ValueError(la.last_error_message())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+
+    def run(self, layer: la.LaKvLayer, q: torch.Tensor, kv_len: torch.Tensor,
+            prefix_len: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """prefix_len: device int32 [n_groups], shared keys of each group."""
+        groups = None
+        if self.cu_group is not None and prefix_len is not None:
+            groups = la.make_prefix_groups(self.cu_group, prefix_len, self.max_group, self.max_prefix_len)
+        la.la_attn_decode(self.shape, layer, q, kv_len, self.max_kv_len, self.o, groups, self.workspace, stream)
+        return self.o
+
+
+class BlockPool:
+    """The blocks of a cache with their table, reference counts and free list
+    (la_block_pool), over tensors the caller holds; BlockPool.new makes an
+    empty one."""
+
+    def __init__(self, cache: torch.Tensor, block_tokens: int, table: torch.Tensor, ref_count: torch.Tensor,
+                 free_list: torch.Tensor, free_count: torch.Tensor, err_count: Optional[torch.Tensor] = None):
+        self.cache, self.block_tokens, self.table = cache, block_tokens, table
+        self.ref_count, self.free_list, self.free_count, self.err_count = ref_count, free_list, free_count, err_count
+        self.pool = la.make_block_pool(cache, block_tokens, table, ref_count, free_list, free_count, err_count)
+        self.workspace = torch.empty(la.la_blocks_compact_workspace_bytes(cache.shape[0]), dtype=torch.uint8,
+                                     device=cache.device)
+
+    @staticmethod
+    def new(n_blocks: int, block_bytes: int, block_tokens: int, n_rows: int, max_blocks: int, device="cuda") -> "BlockPool":
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)
+        return BlockPool(torch.zeros((n_blocks, block_bytes), dtype=torch.uint8, device=device), block_tokens,
+                         i32(n_rows, max_blocks) - 1, i32(n_blocks),
+                         torch.arange(n_blocks - 1, -1, -1, dtype=torch.int32, device=device), i32(1) + n_blocks, i32(1))
+
+    def copy(self, src_ids, dst_ids, stream=None):
+        la.la_blocks_copy(self.pool, src_ids, dst_ids, stream)
+
+    def fork(self, parent_rows, child_rows, lens, stream=None):
+        la.la_blocks_fork(self.pool, parent_rows, child_rows, lens, stream)
+
+    def extend(self, rows, lens, stream=None):
+        la.la_blocks_extend(self.pool, rows, lens, stream)
+
+    def free(self, rows, stream=None):
+        la.la_blocks_free(self.pool, rows, stream)
+
+    def compact(self, new_ids=None, stream=None):
+        la.la_blocks_compact(self.pool, self.workspace, new_ids, stream)

@@ -1,0 +1,218 @@
+// Attention over packed or cached keys: what its kernels share.
+//
+// A row is one (token, query head).  The G = q_heads / kv_heads query heads of
+// a key head stand beside one another, so the rows of a sequence under one key
+// head are numbered token * G + head-in-group and a tile of rows reads each key
+// once for the whole group.  Per row, with c = scale and log2(e) folded in,
+//
+//   t_j = c <q, k_j>,  p_j = 2^(t_j - m),  m = max t_j,  o = sum p_j v_j / sum p_j
+//
+// over the visible keys j < limit(row); a row that sees none is 0.  Keys are
+// taken in tiles with the running m and l = sum p; a part of the keys leaves
+// (m, l, sum p v), and parts join by 2^(m_part - m).  Scores, m, l and the sums
+// are fp32; p is rounded to the type of v for the matrix product (bf16 p: half
+// an ulp, unbiased, of the size of the rounding of the output itself).
+//
+// The kernels form S^T = K Q^T, whose accumulators (rows: keys, columns: rows of
+// q) are the B operand of O^T = V^T P^T as they stand: a lane's accumulators
+// belong to one q row, and the contraction index is permuted on the V side.
+#pragma once
+#include "la_common.h"
+
+namespace la {
+
+typedef unsigned char fp8_t;               // e4m3 bits
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kAttnLog2e = 1.4426950408889634f;
+
+// Where keys and values come from: packed rows, or the blocks of a cache.
+struct KvSource {
+    const char *k, *v;             // packed: first row; cache: the layer's keys / values in block 0
+    int64_t k_stride, v_stride;    // packed: bytes from one token to the next
+    int64_t block_bytes;           // cache: bytes from one block to the next
+    const int32_t *table;          // cache: [sequences, max_blocks]; NULL: packed
+    int64_t max_blocks;
+    int32_t n_blocks, bt_shift;    // blocks of 2^bt_shift tokens
+    int32_t *err;
+};
+
+struct AttnArgs {
+    const void *q;
+    void *o;
+    int64_t q_stride, o_stride;    // elements from one token to the next
+    KvSource kv;
+    const int32_t *cu;             // prompts: token offsets [n_seqs + 1]
+    const int32_t *kv_len;         // keys of each sequence (NULL: as many as its tokens)
+    const int32_t *cu_group;       // decode: sequences of each group [n_groups + 1], or NULL
+    const int32_t *prefix_len;     // decode: shared keys of each group
+    float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
+    int32_t n_seqs, kv_heads, group, n_groups;
+    int32_t max_kv;                // decode: longest kv_len the grid covers
+    int32_t part_tokens;           // decode: keys of one part (prefix; own keys: rows kernel)
+    int32_t parts;                 // parts the workspace holds for each row
+    int32_t group_tiles;           // decode: row tiles of the largest group
+    int32_t prefix_parts;          // decode: of these, the most of a prefix
+    int32_t prefix_part_tokens;
+    float *part_o;                 // [row][parts][D]
+    float2 *part_ml;               // [row][parts]
+};
+
+// --- the sizes of the parts of a prompt's keys ------------------------------
+
+// Keys per part of a sequence of `rows` rows under one key head that reads
+// `keys` keys (a multiple of 64; all keys: not split).
+__host__ __device__ inline int prompt_part_tokens(int64_t rows, int keys) {
+    return keys < 64 ? 64 : (keys + 63) & ~63;
+}
+
+__host__ __device__ inline int prompt_parts(int64_t rows, int keys) {
+    const int t = prompt_part_tokens(rows, keys);
+    return keys <= t ? 1 : (keys + t - 1) / t;
+}
+
+// --- 16-byte pieces of rows, as the LDS tiles hold them ---------------------
+
+template <typename T> struct Piece { static constexpr int N = 16 / sizeof(T); };   // elements
+
+__device__ inline uint2 buf_load8(__amdgpu_buffer_rsrc_t r, uint32_t voff) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)voff, 0, 0);
+    return make_uint2((uint32_t)v[0], (uint32_t)v[1]);
+}
+
+// Four e4m3 values as bf16 pairs (exact).
+__device__ inline uint2 bf16_of_fp8(uint32_t x) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true);
+    return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+
+// The registers of one piece in flight: 16 bytes, or 8 that become 16.
+template <typename C> struct Raw { uint4 x; };
+template <> struct Raw<fp8_t> { uint2 x; };
+
+template <typename C> __device__ inline Raw<C> load_piece(__amdgpu_buffer_rsrc_t r, uint32_t voff) {
+    if constexpr (sizeof(C) == 1) return {buf_load8(r, voff)};
+    else return {buf_load16(r, voff, 0)};
+}
+
+template <typename C> __device__ inline uint4 piece_of(const Raw<C> &p) {
+    if constexpr (sizeof(C) == 1) {
+        const uint2 a = bf16_of_fp8(p.x.x), b = bf16_of_fp8(p.x.y);
+        return make_uint4(a.x, a.y, b.x, b.y);
+    } else {
+        return p.x;
+    }
+}
+
+// Infinities and NaN of a piece made zero; true if there was one.
+template <typename T> __device__ inline bool drop_nonfinite(uint4 &x) {
+    uint32_t *w = &x.x;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            const bool lo = (w[i] & 0x7F80u) == 0x7F80u, hi = (w[i] & 0x7F800000u) == 0x7F800000u;
+            if (lo) w[i] &= 0xFFFF0000u;
+            if (hi) w[i] &= 0x0000FFFFu;
+            any |= lo | hi;
+        } else {
+            const bool bad = (w[i] & 0x7F800000u) == 0x7F800000u;
+            if (bad) w[i] = 0;
+            any |= bad;
+        }
+    }
+    return any;
+}
+
+// Resource over `rows` keys or values (half 0 / 1) from token t on, for one key
+// head: rows at and past `hi` read as zero, as does a block that the table does
+// not name (counted).  The rows lie in one block.  Everything is wave-uniform.
+// HALF_BYTES: bytes of one head's row.
+template <bool PAGED>
+__device__ inline __amdgpu_buffer_rsrc_t kv_rows(const KvSource &s, int half, const int32_t *table_row, int64_t seq_row0,
+                                                 int kvh, int row_bytes, int t, int rows, int hi) {
+    const char *base = half ? s.v : s.k;
+    int n = hi - t;
+    n = n < 0 ? 0 : (n > rows ? rows : n);
+    if constexpr (PAGED) {
+        const int bt = 1 << s.bt_shift;
+        int id = n > 0 ? table_row[t >> s.bt_shift] : 0;
+        if ((uint32_t)id >= (uint32_t)s.n_blocks) {
+            if (half == 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
+            id = 0;
+            n = 0;
+        }
+        const int64_t off = (int64_t)id * s.block_bytes + (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & (bt - 1)));
+        return make_rsrc(base + off, (uint32_t)(n * row_bytes));
+    } else {
+        const int64_t stride = half ? s.v_stride : s.k_stride;
+        const char *p = base + (seq_row0 + t) * stride + (int64_t)kvh * row_bytes;
+        return make_rsrc(n > 0 ? p : base, n > 0 ? (uint32_t)((n - 1) * stride) + (uint32_t)row_bytes : 0u);
+    }
+}
+
+// Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a
+// q row of a 16-column accumulator.
+__device__ inline float row_max16(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float row_sum16(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// Eight (bf16) values of two accumulators as a B operand.
+__device__ inline bf16x8 pack8(f32x4 a, f32x4 b) {
+    return bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3],
+                  (__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
+}
+
+__device__ inline i16x4 lds_tr(const void *p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p);
+}
+
+__device__ inline bf16x8 join_tr(i16x4 a, i16x4 b) {
+    const i16x8 x = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(bf16x8, x);
+}
+
+// Four consecutive outputs.
+__device__ inline void store4(float *p, f32x4 x) { *(f32x4 *)p = x; }
+__device__ inline void store4(__bf16 *p, f32x4 x) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *(bf16x4 *)p = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+}
+
+// The sequence, and the item within it, of item r when sequence i has
+// items(i) of them: every wave computes it, 64 sequences a step.
+template <typename F>
+__device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = i0 + lane;
+        int x = i < n ? items(i) : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        const uint64_t past = __ballot(before + x > r);
+        if (past) {
+            const int at = __ffsll((unsigned long long)past) - 1;
+            const int start = at ? __shfl(x, at - 1) : 0;
+            *seq = __builtin_amdgcn_readfirstlane(i0 + at);
+            *local = __builtin_amdgcn_readfirstlane(r - before - start);
+            return true;
+        }
+        before += __shfl(x, 63);
+    }
+    return false;
+}
+
+}  // namespace la

@@ -15,6 +15,7 @@
 
 #include "linattn.h"
 #include "la_common.h"
+#include "la_host.h"
 #include "gdr_prep.h"
 #include "gdr_scan.h"
 #include "gdr_out.h"
@@ -31,10 +32,11 @@ constexpr size_t kScratchBytes = (size_t)64 << 20;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
 namespace {
-
 thread_local char g_msg[512] = "";
-thread_local void *g_trace[4] = {nullptr, nullptr, nullptr, nullptr};
-thread_local int g_trace_n = 0;
+}  // namespace
+
+namespace la {
+namespace host {
 
 la_status fail(la_status s, const char *fmt, ...) {
     va_list ap;
@@ -50,7 +52,17 @@ la_status hip_check(const char *what) {
     return LA_OK;
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+}  // namespace host
+}  // namespace la
+
+namespace {
+
+using la::host::aligned16;
+using la::host::fail;
+using la::host::hip_check;
+
+thread_local void *g_trace[4] = {nullptr, nullptr, nullptr, nullptr};
+thread_local int g_trace_n = 0;
 
 // Device address of `scratch` on the current device: looked up once per
 // device (with that device current), then reused.  std::call_once makes the

@@ -28,6 +28,7 @@ LA_ERR_WORKSPACE = 6
 
 LA_F32 = 0
 LA_BF16 = 1
+LA_FP8_E4M3 = 2
 LA_GDR_LITERAL = 0
 LA_GDR_DECAYED_DELTA = 1
 
@@ -36,6 +37,9 @@ EXPORTED = ("strict_prefix_boundary", "la_prefill_workspace_bytes", "la_prefill"
             "la_prefill_paged", "la_prefill_paged_noalloc", "la_decode_step", "la_state_save_paged",
             "la_state_restore_paged",
             "la_state_save_host", "la_state_restore_host", "la_hybrid_boundary", "la_hybrid_restore",
+            "la_attn_prefill", "la_attn_prefill_paged", "la_attn_prefill_workspace_bytes", "la_attn_decode",
+            "la_attn_decode_workspace_bytes", "la_kv_write", "la_blocks_copy", "la_blocks_fork", "la_blocks_extend",
+            "la_blocks_free", "la_blocks_compact", "la_blocks_compact_workspace_bytes",
             "la_status_string", "la_last_error_message", "la_trace_set_events")
 
 
@@ -58,6 +62,33 @@ class LaKvBlocks(ctypes.Structure):
                 ("cache", ctypes.c_void_p), ("n_cache_blocks", ctypes.c_int64),
                 ("block_bytes", ctypes.c_int64), ("block_tokens", ctypes.c_int64),
                 ("src_ids", ctypes.c_void_p), ("dst_ids", ctypes.c_void_p), ("max_blocks", ctypes.c_int64)]
+
+
+class LaAttnShape(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o_stride", ctypes.c_int64)]
+
+
+class LaKvLayer(ctypes.Structure):
+    _fields_ = [("cache", ctypes.c_void_p), ("n_blocks", ctypes.c_int64), ("block_bytes", ctypes.c_int64),
+                ("k_offset", ctypes.c_int64), ("v_offset", ctypes.c_int64), ("block_tokens", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("block_table", ctypes.c_void_p),
+                ("max_blocks", ctypes.c_int64), ("err_count", ctypes.c_void_p)]
+
+
+class LaPrefixGroups(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("max_group", ctypes.c_int32), ("cu_group_dev", ctypes.c_void_p),
+                ("prefix_len_dev", ctypes.c_void_p), ("max_prefix_len", ctypes.c_int64)]
+
+
+class LaBlockPool(ctypes.Structure):
+    _fields_ = [("cache", ctypes.c_void_p), ("n_blocks", ctypes.c_int64), ("block_bytes", ctypes.c_int64),
+                ("n_rows", ctypes.c_int64), ("max_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("ref_count", ctypes.c_void_p), ("free_list", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p), ("err_count", ctypes.c_void_p)]
 
 
 def make_shape(n_seqs, n_heads, dk, dv, ckpt_interval, io_dtype=LA_BF16,
@@ -83,6 +114,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     SH = ctypes.POINTER(LaShape)
+    AS, KL, BP = ctypes.POINTER(LaAttnShape), ctypes.POINTER(LaKvLayer), ctypes.POINTER(LaBlockPool)
     sig = {
         "strict_prefix_boundary": ([I64, I64, I64, ctypes.POINTER(I64)], I32),
         "la_prefill_workspace_bytes": ([SH, I64], SZ),
@@ -100,6 +132,18 @@ def _load() -> ctypes.CDLL:
         "la_state_restore_host": ([P, I64, P, P, I64, I64, P, P, P], I32),
         "la_hybrid_boundary": ([I64, I64, I64, I64, I64, ctypes.POINTER(I64), ctypes.POINTER(I64)], I32),
         "la_hybrid_restore": ([ctypes.POINTER(LaKvBlocks), I32, I32, I64, P, P, P, I64, P, P, P, P], I32),
+        "la_attn_prefill": ([AS, P, P, P, P, P, P, P, SZ, P], I32),
+        "la_attn_prefill_paged": ([AS, KL, P, P, P, P, P, P, P, SZ, P], I32),
+        "la_attn_prefill_workspace_bytes": ([AS, P, P], SZ),
+        "la_attn_decode": ([AS, KL, P, P, I64, ctypes.POINTER(LaPrefixGroups), P, P, SZ, P], I32),
+        "la_attn_decode_workspace_bytes": ([AS, I64, I64], SZ),
+        "la_kv_write": ([KL, I32, P, I64, P, I64, P, I32, I64, P, P], I32),
+        "la_blocks_copy": ([BP, P, P, I64, P], I32),
+        "la_blocks_fork": ([BP, P, P, P, I64, P], I32),
+        "la_blocks_extend": ([BP, P, P, I64, P], I32),
+        "la_blocks_free": ([BP, P, I64, P], I32),
+        "la_blocks_compact": ([BP, P, P, SZ, P], I32),
+        "la_blocks_compact_workspace_bytes": ([I64], SZ),
         "la_status_string": ([I32], ctypes.c_char_p),
         "la_last_error_message": ([], ctypes.c_char_p),
         "la_trace_set_events": ([ctypes.POINTER(P), I32], None),
@@ -400,6 +444,243 @@ def la_hybrid_restore(kv: LaKvBlocks, boundary_dev, boundary_host, state_pool, s
     st = _lib.la_hybrid_restore(ctypes.byref(kv), n_seqs, int(n_heads), int(page_elems), _dptr(boundary_dev),
                                 _hptr(bh, np.int64), _anyptr(state_pool), int(n_state_pages),
                                 _dptr(state_page_ids_dev), _dptr(states), _dptr(err_count_dev), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+# ---------------------------------------------------------------------------
+# attention over packed or cached keys, and the cache's blocks
+# ---------------------------------------------------------------------------
+
+def _rows_ptr(t, last) -> Optional[int]:
+    """Device pointer of a [tokens, heads, head_dim] tensor whose heads are
+    packed within a token (a slice of a wider projection will do)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("expected [tokens, heads, head_dim] with packed heads")
+    if last is not None and t.shape[1:] != last:
+        raise ValueError(f"expected heads of shape {tuple(last)}, got {tuple(t.shape[1:])}")
+    return t.data_ptr()
+
+
+def _dtype_of(dtype) -> int:
+    import torch
+    try:
+        return {torch.bfloat16: LA_BF16, torch.float32: LA_F32, torch.float8_e4m3fn: LA_FP8_E4M3}[dtype]
+    except KeyError:
+        raise ValueError(f"no library type for {dtype}") from None
+
+
+def _token_stride(t) -> int:
+    """Elements from one token to the next (0, packed, where there is one token)."""
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _ids(t, what):
+    import torch
+    if t is not None and t.dtype != torch.int32:
+        raise ValueError(f"{what}: expected int32, got {t.dtype}")
+    return t
+
+
+def make_attn_shape(n_seqs, q_heads, kv_heads, head_dim, io_dtype=LA_BF16, scale=None) -> LaAttnShape:
+    """scale None: head_dim ** -0.5.  Token strides are set by each call."""
+    return LaAttnShape(n_seqs, q_heads, kv_heads, head_dim, io_dtype, head_dim ** -0.5 if scale is None else scale,
+                       0, 0, 0, 0)
+
+
+def make_kv_layer(cache, block_table, block_tokens: int, kv_heads: int, head_dim: int, dtype, k_offset: int = 0,
+                  v_offset: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+                  err_count=None) -> LaKvLayer:
+    """la_kv_layer over a byte cache [n_blocks, block_bytes] (uint8) and a device
+    int32 block table [n_seqs, max_blocks].  dtype: torch.bfloat16, float32 or
+    float8_e4m3fn; v_offset None: right behind the keys."""
+    import torch
+    if cache.dim() != 2 or cache.dtype != torch.uint8:
+        raise ValueError("expected a uint8 cache [n_blocks, block_bytes]")
+    if block_table.dim() != 2:
+        raise ValueError("expected a block table [n_seqs, max_blocks]")
+    size = torch.empty(0, dtype=dtype).element_size()
+    if v_offset is None:
+        v_offset = k_offset + kv_heads * block_tokens * head_dim * size
+    y = LaKvLayer(_dptr(cache), cache.shape[0], cache.shape[1], k_offset, v_offset, block_tokens, kv_heads, head_dim,
+                  _dtype_of(dtype), k_scale, v_scale, _dptr(_ids(block_table, "block_table")), block_table.shape[1],
+                  _dptr(_ids(err_count, "err_count")))
+    y._keep = (cache, block_table, err_count)       # the struct holds raw addresses only
+    y._seqs = block_table.shape[0]
+    return y
+
+
+def make_prefix_groups(cu_group, prefix_len, max_group: int, max_prefix_len: int) -> LaPrefixGroups:
+    """la_prefix_groups from device int32 tensors [n_groups + 1] and [n_groups]."""
+    n = prefix_len.numel()
+    if cu_group.numel() != n + 1:
+        raise ValueError(f"{n} prefix lengths go with {n + 1} group offsets")
+    g = LaPrefixGroups(n, int(max_group), _dptr(_ids(cu_group, "cu_group")), _dptr(_ids(prefix_len, "prefix_len")),
+                       int(max_prefix_len))
+    g._keep = (cu_group, prefix_len)
+    return g
+
+
+def make_block_pool(cache, block_tokens: int, table, ref_count, free_list, free_count, err_count=None) -> LaBlockPool:
+    """la_block_pool over a uint8 cache [n_blocks, block_bytes] and device int32
+    table [rows, max_blocks], ref_count, free_list [n_blocks] and free_count [1]."""
+    import torch
+    if cache.dim() != 2 or cache.dtype != torch.uint8:
+        raise ValueError("expected a uint8 cache [n_blocks, block_bytes]")
+    if table.dim() != 2:
+        raise ValueError("expected a block table [rows, max_blocks]")
+    if ref_count.numel() != cache.shape[0] or free_list.numel() != cache.shape[0] or free_count.numel() != 1:
+        raise ValueError("expected ref_count and free_list with one entry a block, free_count with one")
+    p = LaBlockPool(_dptr(cache), cache.shape[0], cache.shape[1], table.shape[0], table.shape[1], block_tokens,
+                    _dptr(_ids(table, "table")), _dptr(_ids(ref_count, "ref_count")),
+                    _dptr(_ids(free_list, "free_list")), _dptr(_ids(free_count, "free_count")),
+                    _dptr(_ids(err_count, "err_count")))
+    p._keep = (cache, table, ref_count, free_list, free_count, err_count)
+    return p
+
+
+def _with_strides(shape: LaAttnShape, q, k, v, o) -> LaAttnShape:
+    shape.q_stride, shape.o_stride = _token_stride(q), _token_stride(o)
+    shape.k_stride = 0 if k is None else _token_stride(k)
+    shape.v_stride = 0 if v is None else _token_stride(v)
+    return shape
+
+
+def _attn_io(shape: LaAttnShape, q, o, rows):
+    want = (shape.q_heads, shape.head_dim)
+    if _dtype_of(q.dtype) != shape.io_dtype or o.dtype != q.dtype:
+        raise ValueError("q and o must have the shape's io_dtype")
+    if q.shape[0] != rows or o.shape[0] != rows:
+        raise ValueError(f"q and o must have {rows} rows")
+    return _rows_ptr(q, want), _rows_ptr(o, want)
+
+
+def _ws(workspace):
+    return (0, 0) if workspace is None else (_dptr(workspace), workspace.numel() * workspace.element_size())
+
+
+def la_attn_prefill_workspace_bytes(shape: LaAttnShape, cu_host: np.ndarray, kv_len_host=None) -> int:
+    return _lib.la_attn_prefill_workspace_bytes(ctypes.byref(shape), _hptr(cu_host, np.int32),
+                                                _hptr(kv_len_host, np.int32))
+
+
+def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o, workspace=None, stream=None,
+                    check: bool = True) -> int:
+    """q, o [T, q_heads, d], k, v [T, kv_heads, d]: heads packed, tokens at any stride."""
+    T = int(cu_host[shape.n_seqs])
+    qp, op = _attn_io(shape, q, o, T)
+    if k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != T or v.shape[0] != T:
+        raise ValueError(f"k and v must have q's type and {T} rows")
+    kv = (shape.kv_heads, shape.head_dim)
+    w, n = _ws(workspace)
+    st = _lib.la_attn_prefill(ctypes.byref(_with_strides(shape, q, k, v, o)), qp, _rows_ptr(k, kv), _rows_ptr(v, kv),
+                              _dptr(_ids(cu_dev, "cu_seqlens")), _hptr(cu_host, np.int32), op, w, n, _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_attn_prefill_paged(shape: LaAttnShape, layer: LaKvLayer, q, cu_dev, cu_host: np.ndarray, kv_len_dev,
+                          kv_len_host: np.ndarray, o, workspace=None, stream=None, check: bool = True) -> int:
+    qp, op = _attn_io(shape, q, o, int(cu_host[shape.n_seqs]))
+    if layer._seqs < shape.n_seqs:
+        raise ValueError("the block table has fewer rows than the call sequences")
+    w, n = _ws(workspace)
+    st = _lib.la_attn_prefill_paged(ctypes.byref(_with_strides(shape, q, None, None, o)), ctypes.byref(layer), qp,
+                                    _dptr(_ids(cu_dev, "cu_seqlens")), _hptr(cu_host, np.int32),
+                                    _dptr(_ids(kv_len_dev, "kv_len")), _hptr(kv_len_host, np.int32), op, w, n,
+                                    _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_attn_decode_workspace_bytes(shape: LaAttnShape, max_kv_len: int, max_prefix_len: int = 0) -> int:
+    return _lib.la_attn_decode_workspace_bytes(ctypes.byref(shape), int(max_kv_len), int(max_prefix_len))
+
+
+def la_attn_decode(shape: LaAttnShape, layer: LaKvLayer, q, kv_len_dev, max_kv_len: int, o,
+                   groups: Optional[LaPrefixGroups] = None, workspace=None, stream=None, check: bool = True) -> int:
+    qp, op = _attn_io(shape, q, o, shape.n_seqs)
+    if layer._seqs < shape.n_seqs or kv_len_dev.numel() < shape.n_seqs:
+        raise ValueError("the block table or kv_len has fewer rows than the call sequences")
+    w, n = _ws(workspace)
+    st = _lib.la_attn_decode(ctypes.byref(_with_strides(shape, q, None, None, o)), ctypes.byref(layer), qp,
+                             _dptr(_ids(kv_len_dev, "kv_len")), int(max_kv_len),
+                             None if groups is None else ctypes.byref(groups), op, w, n, _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_kv_write(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: bool = True) -> int:
+    """k, v [T, kv_heads, d] into the cache blocks of the sequences of cu_dev [n_seqs + 1]."""
+    n_seqs = cu_dev.numel() - 1
+    if k.dtype != v.dtype or k.shape != v.shape:
+        raise ValueError("k and v must have one type and shape")
+    if layer._seqs < n_seqs or kv_len_dev.numel() < n_seqs:
+        raise ValueError("the block table or kv_len has fewer rows than the call sequences")
+    kv = (layer.kv_heads, layer.head_dim)
+    st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(k.dtype), _rows_ptr(k, kv), _token_stride(k), _rows_ptr(v, kv),
+                          _token_stride(v), _dptr(_ids(cu_dev, "cu_seqlens")), n_seqs, k.shape[0],
+                          _dptr(_ids(kv_len_dev, "kv_len")), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def _same_count(*lists):
+    if len({t.numel() for t in lists}) != 1:
+        raise ValueError("lists of one length are expected")
+    return lists[0].numel()
+
+
+def la_blocks_copy(pool: LaBlockPool, src_ids, dst_ids, stream=None, check: bool = True) -> int:
+    st = _lib.la_blocks_copy(ctypes.byref(pool), _dptr(_ids(src_ids, "src_ids")), _dptr(_ids(dst_ids, "dst_ids")),
+                             _same_count(src_ids, dst_ids), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_blocks_fork(pool: LaBlockPool, parent_rows, child_rows, lens, stream=None, check: bool = True) -> int:
+    st = _lib.la_blocks_fork(ctypes.byref(pool), _dptr(_ids(parent_rows, "parent_rows")),
+                             _dptr(_ids(child_rows, "child_rows")), _dptr(_ids(lens, "lens")),
+                             _same_count(parent_rows, child_rows, lens), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_blocks_extend(pool: LaBlockPool, rows, lens, stream=None, check: bool = True) -> int:
+    st = _lib.la_blocks_extend(ctypes.byref(pool), _dptr(_ids(rows, "rows")), _dptr(_ids(lens, "lens")),
+                               _same_count(rows, lens), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_blocks_free(pool: LaBlockPool, rows, stream=None, check: bool = True) -> int:
+    st = _lib.la_blocks_free(ctypes.byref(pool), _dptr(_ids(rows, "rows")), rows.numel(), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_blocks_compact_workspace_bytes(n_blocks: int) -> int:
+    return _lib.la_blocks_compact_workspace_bytes(int(n_blocks))
+
+
+def la_blocks_compact(pool: LaBlockPool, workspace, new_ids=None, stream=None, check: bool = True) -> int:
+    w, n = _ws(workspace)
+    if new_ids is not None and new_ids.numel() != pool.n_blocks:
+        raise ValueError("expected new_ids with one entry a block")
+    st = _lib.la_blocks_compact(ctypes.byref(pool), _dptr(_ids(new_ids, "new_ids")), w, n, _stream(stream))
     if check:
         _check(st)
     return st

@@ -1,0 +1,184 @@
+"""The attention and block entry points on the CPU: what they refuse before any
+launch, and their workspace sizes.  Device pointers here are dummies that
+validation never dereferences."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2609_15030_amd import linattn as la
+
+P = 0x10000                    # a 16-byte aligned address
+LIB = la.library()
+
+
+def _shape(**kw):
+    s = la.make_attn_shape(2, 8, 2, 128)
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+def _layer(**kw):
+    y = la.LaKvLayer(P, 100, 65536, 0, 8192, 16, 2, 128, la.LA_BF16, 1.0, 1.0, P, 40, None)
+    for k, v in kw.items():
+        setattr(y, k, v)
+    return y
+
+
+def _cu(*v):
+    return np.array(v, np.int32)
+
+
+def _ptr(a):
+    return None if a is None else a.ctypes.data
+
+
+def _prefill(s, cu=_cu(0, 30, 700), q=P, k=P, v=P, o=P, cu_dev=P, ws=P, n=1 << 30):
+    return LIB.la_attn_prefill(ctypes.byref(s), q, k, v, cu_dev, _ptr(cu), o, ws, n, None)
+
+
+def _paged(s, y, cu=_cu(0, 30, 60), kv=_cu(30, 600), q=P, o=P, kv_dev=P, ws=P, n=1 << 30):
+    return LIB.la_attn_prefill_paged(ctypes.byref(s), ctypes.byref(y), q, P, _ptr(cu), kv_dev, _ptr(kv), o, ws, n, None)
+
+
+def _decode(s, y, kv=600, groups=None, q=P, o=P, kv_dev=P, ws=P, n=1 << 40):
+    return LIB.la_attn_decode(ctypes.byref(s), ctypes.byref(y), q, kv_dev, kv, None if groups is None else ctypes.byref(groups), o,
+                              ws, n, None)
+
+
+BAD_SHAPES = [
+    (dict(n_seqs=0), la.LA_ERR_INVALID_ARG), (dict(kv_heads=0), la.LA_ERR_INVALID_ARG),
+    (dict(q_heads=7), la.LA_ERR_INVALID_ARG), (dict(head_dim=96), la.LA_ERR_UNSUPPORTED),
+    (dict(io_dtype=la.LA_FP8_E4M3), la.LA_ERR_INVALID_ARG), (dict(scale=0.0), la.LA_ERR_INVALID_ARG),
+    (dict(scale=-1.0), la.LA_ERR_INVALID_ARG), (dict(scale=float("nan")), la.LA_ERR_INVALID_ARG),
+    (dict(scale=float("inf")), la.LA_ERR_INVALID_ARG), (dict(q_stride=1000), la.LA_ERR_INVALID_ARG),
+    (dict(q_stride=1028), la.LA_ERR_INVALID_ARG), (dict(o_stride=1 << 25), la.LA_ERR_INVALID_ARG),
+]
+
+
+@pytest.mark.parametrize("change,want", BAD_SHAPES, ids=lambda x: str(x))
+def test_shapes_are_refused(change, want):
+    s = _shape(**change)
+    assert _prefill(s) == want
+    assert _paged(s, _layer()) == want
+    assert _decode(s, _layer()) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(dtype=7), la.LA_ERR_INVALID_ARG), (dict(dtype=la.LA_F32), la.LA_ERR_UNSUPPORTED),
+    (dict(kv_heads=4), la.LA_ERR_INVALID_ARG), (dict(head_dim=64), la.LA_ERR_INVALID_ARG),
+    (dict(head_dim=80), la.LA_ERR_UNSUPPORTED), (dict(block_tokens=8), la.LA_ERR_UNSUPPORTED),
+    (dict(block_tokens=48), la.LA_ERR_UNSUPPORTED), (dict(block_tokens=512), la.LA_ERR_UNSUPPORTED),
+    (dict(n_blocks=-1), la.LA_ERR_INVALID_ARG), (dict(block_bytes=16000), la.LA_ERR_INVALID_ARG),
+    (dict(v_offset=8), la.LA_ERR_INVALID_ARG), (dict(v_offset=4096), la.LA_ERR_INVALID_ARG),
+    (dict(k_offset=-16), la.LA_ERR_INVALID_ARG), (dict(v_offset=65536 - 4096), la.LA_ERR_INVALID_ARG),
+    (dict(k_scale=0.0), la.LA_ERR_INVALID_ARG), (dict(k_scale=2.0), la.LA_ERR_INVALID_ARG),
+    (dict(v_scale=float("inf")), la.LA_ERR_INVALID_ARG), (dict(max_blocks=0), la.LA_ERR_INVALID_ARG),
+    (dict(max_blocks=1 << 28), la.LA_ERR_INVALID_ARG), (dict(block_table=None), la.LA_ERR_INVALID_ARG),
+    (dict(cache=None), la.LA_ERR_INVALID_ARG), (dict(cache=P + 8), la.LA_ERR_INVALID_ARG),
+], ids=lambda x: str(x))
+def test_layers_are_refused(change, want):
+    y = _layer(**change)
+    assert _paged(_shape(), y) == want
+    assert _decode(_shape(), y) == want
+    if "kv_heads" not in change and change != dict(head_dim=64):     # a write has no shape to disagree with
+        assert LIB.la_kv_write(ctypes.byref(y), la.LA_BF16, P, 0, P, 0, P, 2, 10, P, None) == want
+
+
+def test_lengths_and_pointers_are_refused():
+    s, y = _shape(), _layer()
+    assert _prefill(s, cu=None) == la.LA_ERR_INVALID_ARG
+    assert _prefill(s, cu=_cu(1, 2, 3)) == la.LA_ERR_INVALID_ARG
+    assert _prefill(s, cu=_cu(0, 5, 4)) == la.LA_ERR_INVALID_ARG
+    assert _prefill(s, cu=_cu(0, 0, 1 << 30)) == la.LA_ERR_INVALID_ARG
+    for name in ("q", "k", "v", "o", "cu_dev"):
+        assert _prefill(s, **{name: None}) == la.LA_ERR_INVALID_ARG, name
+    for name in ("q", "k", "v", "o"):
+        assert _prefill(s, **{name: P + 2}) == la.LA_ERR_INVALID_ARG, name
+    assert _prefill(_shape(k_stride=128), ) == la.LA_ERR_INVALID_ARG
+    assert _prefill(s, cu=_cu(0, 0, 0), q=None) == la.LA_OK           # no token: nothing to do
+    assert _paged(s, y, kv=None) == la.LA_ERR_INVALID_ARG
+    assert _paged(s, y, kv=_cu(30, -1)) == la.LA_ERR_INVALID_ARG
+    assert _paged(s, y, kv=_cu(30, 641)) == la.LA_ERR_INVALID_ARG     # the table covers 640 tokens
+    assert _paged(s, y, kv_dev=None) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, kv=641) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, kv=-1) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, kv_dev=None) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, q=None) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, ws=None) == la.LA_ERR_WORKSPACE
+    assert _decode(s, y, n=16) == la.LA_ERR_WORKSPACE
+    assert _decode(s, y, ws=P + 4) == la.LA_ERR_INVALID_ARG
+    g = lambda *a: la.LaPrefixGroups(*a)
+    assert _decode(s, y, groups=g(-1, 1, P, P, 0)) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, groups=g(1, 2, None, P, 64)) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, groups=g(1, 3, P, P, 64)) == la.LA_ERR_INVALID_ARG
+    assert _decode(s, y, groups=g(1, 2, P, P, 601)) == la.LA_ERR_INVALID_ARG
+    w = lambda dt=la.LA_BF16, k=P, ks=0, seqs=2, toks=10: LIB.la_kv_write(ctypes.byref(y), dt, k, ks, P, 0, P, seqs, toks, P, None)
+    assert w(dt=la.LA_F32) == la.LA_ERR_UNSUPPORTED
+    assert w(dt=5) == la.LA_ERR_INVALID_ARG
+    assert w(k=None) == la.LA_ERR_INVALID_ARG
+    assert w(k=P + 8) == la.LA_ERR_INVALID_ARG
+    assert w(ks=100) == la.LA_ERR_INVALID_ARG
+    assert w(toks=-1) == la.LA_ERR_INVALID_ARG
+    assert w(toks=0, k=None) == la.LA_OK
+    assert "k_stride" in la.last_error_message() or la.last_error_message()
+
+
+def test_pools_are_refused():
+    def pool(**kw):
+        p = la.LaBlockPool(P, 100, 4096, 8, 10, 16, P, P, P, P, None)
+        for k, v in kw.items():
+            setattr(p, k, v)
+        return ctypes.byref(p)
+
+    fork = lambda p, n=2, a=P, b=P, c=P: LIB.la_blocks_fork(p, a, b, c, n, None)
+    bad = la.LA_ERR_INVALID_ARG
+    for change in (dict(n_blocks=-1), dict(block_bytes=0), dict(block_bytes=24), dict(block_bytes=1 << 32), dict(cache=None),
+                   dict(cache=P + 4)):
+        assert fork(pool(**change)) == bad, change
+        assert LIB.la_blocks_copy(pool(**change), P, P, 3, None) == bad, change
+        assert LIB.la_blocks_compact(pool(**change), None, P, 1 << 20, None) == bad, change
+    for change in (dict(block_tokens=0), dict(block_tokens=12), dict(n_rows=-1), dict(max_blocks=0), dict(max_blocks=1 << 30),
+                   dict(table=None), dict(ref_count=None), dict(free_list=None), dict(free_count=None)):
+        assert fork(pool(**change)) == bad, change
+        assert LIB.la_blocks_extend(pool(**change), P, P, 3, None) == bad, change
+        assert LIB.la_blocks_free(pool(**change), P, 3, None) == bad, change
+        assert LIB.la_blocks_compact(pool(**change), None, P, 1 << 20, None) == bad, change
+    assert fork(pool(), n=-1) == bad and fork(pool(), n=65536) == bad
+    assert fork(pool(), a=None) == bad and fork(pool(), b=None) == bad and fork(pool(), c=None) == bad
+    assert fork(pool(), n=0) == la.LA_OK
+    assert LIB.la_blocks_extend(pool(), P, None, 3, None) == bad
+    assert LIB.la_blocks_free(pool(), None, 3, None) == bad
+    assert LIB.la_blocks_copy(pool(), P, None, 3, None) == bad
+    assert LIB.la_blocks_copy(pool(), P, P, -1, None) == bad
+    assert LIB.la_blocks_compact(pool(), None, None, 1 << 20, None) == la.LA_ERR_WORKSPACE
+    assert LIB.la_blocks_compact(pool(), None, P, 100, None) == la.LA_ERR_WORKSPACE
+    assert LIB.la_blocks_compact(pool(), None, P + 2, 1 << 20, None) == bad
+
+
+def test_workspace_sizes():
+    s = _shape()
+    assert la.la_attn_prefill_workspace_bytes(s, _cu(0, 30, 700)) > 0
+    assert la.la_attn_prefill_workspace_bytes(_shape(head_dim=32), _cu(0, 30, 700)) == 0
+    assert la.la_attn_prefill_workspace_bytes(s, _cu(0, 30, 20)) == 0
+    a = la.la_attn_decode_workspace_bytes(s, 4000)
+    assert 0 < a <= la.la_attn_decode_workspace_bytes(s, 8000) <= la.la_attn_decode_workspace_bytes(s, 8000, 4000)
+    assert la.la_attn_decode_workspace_bytes(s, -1) == 0
+    assert la.la_blocks_compact_workspace_bytes(-1) == 0
+    assert la.la_blocks_compact_workspace_bytes(5000) >= 3 * 5000 * 4
+
+
+def test_binding_refuses_wrong_tensors():
+    import torch
+    cache, table = torch.zeros((4, 65536), dtype=torch.uint8), torch.zeros((1, 4), dtype=torch.int32)
+    with pytest.raises(ValueError):          # host memory
+        la.make_kv_layer(cache, table, 16, 2, 128, torch.bfloat16)
+    with pytest.raises(ValueError):
+        la.make_kv_layer(cache.float(), table, 16, 2, 128, torch.bfloat16)
+    with pytest.raises(ValueError):
+        la.make_kv_layer(cache, table[0], 16, 2, 128, torch.bfloat16)
+    with pytest.raises(ValueError):
+        la._dtype_of(torch.float16)
+    with pytest.raises(ValueError):
+        la._ids(table.long(), "table")
