@@ -105,28 +105,42 @@ la::KvSource cached(const la_kv_layer *y) {
 
 // --- prompts -----------------------------------------------------------------
 
+// Workgroups that a call of whole rows should have before its keys are left
+// unsplit: one on every CU.
+constexpr int64_t kFullGrid = 256;
+
 struct PromptPlan {
     int64_t tokens = 0, items = 0;      // items: row tiles times parts, of one key head
     int parts = 1;                      // the most parts of a sequence
     int32_t max_kv = 0;
+    int waves = 8;                      // of a workgroup: 16 rows each
 };
 
-la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *kv_len, int rows_per_tile, PromptPlan *p) {
+la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *kv_len, PromptPlan *p) {
     if (!cu) return fail(LA_ERR_INVALID_ARG, "cu_seqlens_host is required");
     if (cu[0] != 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens[0]=%d", cu[0]);
     const int64_t group = s->q_heads / s->kv_heads;
+    auto keys_of = [&](int i) { return kv_len ? kv_len[i] : cu[i + 1] - cu[i]; };
+    auto tiles = [&](int rows_per_tile, bool split) {
+        int64_t n = 0;
+        for (int i = 0; i < s->n_seqs; ++i)
+            n += up((cu[i + 1] - cu[i]) * group, rows_per_tile) * la::prompt_parts(split, keys_of(i));
+        return n;
+    };
     for (int i = 0; i < s->n_seqs; ++i) {
         const int64_t n = (int64_t)cu[i + 1] - cu[i];
         if (n < 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens decreases at sequence %d", i);
         if (n * group > 0x7fffff00) return fail(LA_ERR_INVALID_ARG, "sequence %d is too long for one launch", i);
-        const int64_t keys = kv_len ? kv_len[i] : n;
-        if (keys < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%lld", i, (long long)keys);
-        const int parts = la::prompt_parts(n * group, (int)keys);
-        p->items += up(n * group, rows_per_tile) * parts;
-        p->parts = std::max(p->parts, n ? parts : 1);
-        p->max_kv = std::max(p->max_kv, (int32_t)keys);
+        if (keys_of(i) < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys_of(i));
+        p->max_kv = std::max(p->max_kv, keys_of(i));
     }
     p->tokens = cu[s->n_seqs];
+    p->waves = tiles(128, false) * s->kv_heads < kFullGrid ? 4 : 8;
+    p->items = tiles(16 * p->waves, false);
+    if (p->items * s->kv_heads < kFullGrid && p->max_kv > la::kPromptPart) {
+        p->parts = la::prompt_parts(true, p->max_kv);
+        p->items = tiles(16 * p->waves, true);
+    }
     if (p->items * s->kv_heads > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "too many row tiles for one launch");
     return LA_OK;
 }
@@ -139,32 +153,20 @@ void carve_parts(la::AttnArgs *a, void *ws, int64_t rows, int d) {
 }
 
 template <typename T, typename C, int D, bool PAGED>
-la_status launch_tiles(const la::AttnArgs &a, int64_t items, hipStream_t st) {
-    hipLaunchKernelGGL((la::attn_tile_kernel<T, C, D, PAGED>), dim3((unsigned)(items * a.kv_heads)), dim3(la::kTileThreads), 0, st, a);
-    return hip_check("attention tile launch");
-}
-
-template <typename T, typename C, bool PAGED>
-la_status tiles_of_dim(int d, const la::AttnArgs &a, int64_t items, hipStream_t st) {
-    return d == 64 ? launch_tiles<T, C, 64, PAGED>(a, items, st) : launch_tiles<T, C, 128, PAGED>(a, items, st);
-}
-
-la_status launch_tiles_paged(const la_attn_shape *s, int32_t cache, const la::AttnArgs &a, int64_t items, hipStream_t st) {
-    if (cache == LA_F32) return tiles_of_dim<float, float, true>(s->head_dim, a, items, st);
-    if (cache == LA_BF16) return tiles_of_dim<__bf16, __bf16, true>(s->head_dim, a, items, st);
-    return tiles_of_dim<__bf16, la::fp8_t, true>(s->head_dim, a, items, st);
-}
-
-template <typename T>
-la_status launch_join(int d, const la::AttnArgs &a, int64_t rows, hipStream_t st) {
-    const dim3 grid((unsigned)up(rows, 4));
-    if (d == 64) hipLaunchKernelGGL((la::attn_join_kernel<T, 64>), grid, dim3(256), 0, st, a, rows);
-    else hipLaunchKernelGGL((la::attn_join_kernel<T, 128>), grid, dim3(256), 0, st, a, rows);
+la_status launch_prompt(const la::AttnArgs &a, const PromptPlan &p, hipStream_t st) {
+    const dim3 grid((unsigned)(p.items * a.kv_heads));
+    if (p.waves == 4) hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 4>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 8>), grid, dim3(512), 0, st, a);
+    if (la_status e = hip_check("attention prompt launch")) return e;
+    if (!a.split) return LA_OK;
+    const int64_t rows = p.tokens * a.kv_heads * a.group;
+    hipLaunchKernelGGL((la::attn_join_prompt_kernel<T, D>), dim3((unsigned)up(rows, 256 / (D / 4))), dim3(256), 0, st, a, rows);
     return hip_check("attention join launch");
 }
 
-la_status join_rows(const la_attn_shape *s, const la::AttnArgs &a, int64_t rows, hipStream_t st) {
-    return s->io_dtype == LA_F32 ? launch_join<float>(s->head_dim, a, rows, st) : launch_join<__bf16>(s->head_dim, a, rows, st);
+template <typename T, typename C, bool PAGED>
+la_status prompt_of_dim(int d, const la::AttnArgs &a, const PromptPlan &p, hipStream_t st) {
+    return d == 64 ? launch_prompt<T, C, 64, PAGED>(a, p, st) : launch_prompt<T, C, 128, PAGED>(a, p, st);
 }
 
 la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer *layer, const PromptPlan &p, void *ws,
@@ -177,15 +179,16 @@ la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer 
     a.group = s->q_heads / s->kv_heads;
     a.n_seqs = s->n_seqs;
     a.parts = p.parts;
+    a.split = p.parts > 1;
     a.max_kv = p.max_kv;
     carve_parts(&a, ws, p.tokens * s->q_heads, s->head_dim);
     (void)hipGetLastError();
-    la_status e;
-    if (layer) e = launch_tiles_paged(s, layer->dtype, a, p.items, st);
-    else if (s->io_dtype == LA_F32) e = tiles_of_dim<float, float, false>(s->head_dim, a, p.items, st);
-    else e = tiles_of_dim<__bf16, __bf16, false>(s->head_dim, a, p.items, st);
-    if (e || p.parts == 1) return e;
-    return join_rows(s, a, p.tokens * s->q_heads, st);
+    const int d = s->head_dim;
+    if (!layer)
+        return s->io_dtype == LA_F32 ? prompt_of_dim<float, float, false>(d, a, p, st) : prompt_of_dim<__bf16, __bf16, false>(d, a, p, st);
+    if (layer->dtype == LA_F32) return prompt_of_dim<float, float, true>(d, a, p, st);
+    if (layer->dtype == LA_BF16) return prompt_of_dim<__bf16, __bf16, true>(d, a, p, st);
+    return prompt_of_dim<__bf16, la::fp8_t, true>(d, a, p, st);
 }
 
 la_status check_qo(const la_attn_shape *s, const void *q, const void *o, la::AttnArgs *a) {
@@ -200,21 +203,17 @@ la_status check_qo(const la_attn_shape *s, const void *q, const void *o, la::Att
 
 // --- decode ------------------------------------------------------------------
 
-constexpr int kOwnPart = 512;          // keys of one part of a sequence's own keys
-constexpr int kPrefixPart = 512;       // and of a shared prefix
+constexpr int kRowsGrid = 512;         // workgroups for own keys: two on every CU
 
 struct DecodePlan {
-    int own_parts, prefix_parts, own_tokens, prefix_tokens;
-    bool direct;
+    int own_parts, prefix_parts;
+    bool direct;                       // one part each: no join
 };
 
 DecodePlan plan_decode(int64_t max_kv_len, int64_t max_prefix) {
     DecodePlan p{};
-    p.own_tokens = kOwnPart;
-    p.prefix_tokens = kPrefixPart;
-    // own keys begin on the 16-token line before the first
-    p.own_parts = (int)std::max<int64_t>(1, up(max_kv_len, kOwnPart));
-    p.prefix_parts = (int)up(max_prefix, kPrefixPart);
+    p.own_parts = (int)std::max<int64_t>(1, up(max_kv_len, la::kOwnPart));
+    p.prefix_parts = (int)up(max_prefix, la::kPrefixPart);
     p.direct = p.own_parts == 1 && p.prefix_parts == 0;
     return p;
 }
@@ -227,14 +226,18 @@ la_status check_decode_sizes(const la_attn_shape *s, int64_t max_kv_len, int64_t
 }
 
 template <typename T, typename C, int D>
-la_status launch_rows(const la::AttnArgs &a, int64_t blocks, bool direct, hipStream_t st) {
-    hipLaunchKernelGGL((la::attn_rows_kernel<T, C, D>), dim3((unsigned)blocks), dim3(la::kRowsThreads), 0, st, a, direct);
-    return hip_check("attention row launch");
+la_status launch_decode(const la::AttnArgs &a, int64_t rows_blocks, hipStream_t st) {
+    hipLaunchKernelGGL((la::attn_decode_kernel<T, C, D>), dim3((unsigned)(a.prefix_items + rows_blocks)), dim3(la::kDecodeThreads8), 0,
+                       st, a);
+    if (la_status e = hip_check("attention decode launch")) return e;
+    if (a.direct) return LA_OK;
+    hipLaunchKernelGGL((la::attn_join_kernel<T, D>), dim3((unsigned)(a.n_seqs * a.kv_heads * a.group)), dim3(256), 0, st, a);
+    return hip_check("attention join launch");
 }
 
 template <typename T, typename C>
-la_status rows_of_dim(int d, const la::AttnArgs &a, int64_t blocks, bool direct, hipStream_t st) {
-    return d == 64 ? launch_rows<T, C, 64>(a, blocks, direct, st) : launch_rows<T, C, 128>(a, blocks, direct, st);
+la_status decode_of_dim(int d, const la::AttnArgs &a, int64_t rows_blocks, hipStream_t st) {
+    return d == 64 ? launch_decode<T, C, 64>(a, rows_blocks, st) : launch_decode<T, C, 128>(a, rows_blocks, st);
 }
 
 // --- blocks ------------------------------------------------------------------
@@ -289,7 +292,7 @@ extern "C" {
 
 size_t la_attn_prefill_workspace_bytes(const la_attn_shape *shape, const int32_t *cu_seqlens_host, const int32_t *kv_len_host) {
     PromptPlan p;
-    if (check_attn_shape(shape) || plan_prompt(shape, cu_seqlens_host, kv_len_host, la::kTileRows, &p)) return 0;
+    if (check_attn_shape(shape) || plan_prompt(shape, cu_seqlens_host, kv_len_host, &p)) return 0;
     return p.parts > 1 ? parts_bytes(p.tokens * shape->q_heads, p.parts, shape->head_dim) : 16;
 }
 
@@ -297,7 +300,7 @@ la_status la_attn_prefill(const la_attn_shape *shape, const void *q, const void 
                           const int32_t *cu_seqlens_host, void *o, void *workspace, size_t ws_bytes, void *stream) {
     if (la_status e = check_attn_shape(shape)) return e;
     PromptPlan p;
-    if (la_status e = plan_prompt(shape, cu_seqlens_host, nullptr, la::kTileRows, &p)) return e;
+    if (la_status e = plan_prompt(shape, cu_seqlens_host, nullptr, &p)) return e;
     if (p.tokens == 0) return LA_OK;
     la::AttnArgs a{};
     if (la_status e = check_qo(shape, q, o, &a)) return e;
@@ -323,7 +326,7 @@ la_status la_attn_prefill_paged(const la_attn_shape *shape, const la_kv_layer *l
     if (la_status e = check_layer_of(layer, shape)) return e;
     if (!kv_len_host) return fail(LA_ERR_INVALID_ARG, "kv_len_host is required");
     PromptPlan p;
-    if (la_status e = plan_prompt(shape, cu_seqlens_host, kv_len_host, la::kTileRows, &p)) return e;
+    if (la_status e = plan_prompt(shape, cu_seqlens_host, kv_len_host, &p)) return e;
     if (p.tokens == 0) return LA_OK;
     if (p.max_kv > layer->max_blocks * layer->block_tokens)
         return fail(LA_ERR_INVALID_ARG, "kv_len reaches %d, the block table %lld tokens", p.max_kv,
@@ -365,6 +368,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
         return fail(LA_ERR_INVALID_ARG, "max_group=%d of %d sequences", groups->max_group, shape->n_seqs);
     const DecodePlan p = plan_decode(max_kv_len, max_prefix);
     a.parts = p.own_parts + p.prefix_parts;
+    a.direct = p.direct;
     const int64_t rows = (int64_t)shape->n_seqs * shape->q_heads;
     const size_t need = p.direct ? 0 : parts_bytes(rows, a.parts, shape->head_dim);
     if (need && (!workspace || ws_bytes < need))
@@ -378,30 +382,26 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     a.kv_heads = shape->kv_heads;
     a.group = shape->q_heads / shape->kv_heads;
     a.max_kv = (int32_t)max_kv_len;
-    a.part_tokens = p.own_tokens;
-    a.prefix_parts = p.prefix_parts;
-    a.prefix_part_tokens = p.prefix_tokens;
     carve_parts(&a, workspace, rows, shape->head_dim);
-    const int64_t blocks = rows / a.group * up(a.group, la::kRowsHeads) * p.own_parts;
+    const int64_t items = rows / a.group * up(a.group, la::kRowsHeads) * p.own_parts;
     int64_t prefix_items = 0;
     if (shared) {
         a.cu_group = groups->cu_group_dev;
         a.prefix_len = groups->prefix_len_dev;
         a.n_groups = groups->n_groups;
-        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, la::kTileRows);
-        prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups;
+        a.prefix_parts = p.prefix_parts;
+        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, 16 * la::kDecodeWaves);
+        prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups * a.kv_heads;
     }
-    if (blocks > kMaxGrid || prefix_items * a.kv_heads > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "too many parts for one launch");
+    if (items > kMaxGrid || rows > kMaxGrid || prefix_items + kRowsGrid > kMaxGrid)
+        return fail(LA_ERR_INVALID_ARG, "too many parts for one launch");
+    a.prefix_items = (int32_t)prefix_items;
+    const int64_t blocks = std::min<int64_t>(items, kRowsGrid);
     hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
-    if (shared)
-        if (la_status e = launch_tiles_paged(shape, layer->dtype, a, prefix_items, st)) return e;
-    la_status e;
-    if (layer->dtype == LA_F32) e = rows_of_dim<float, float>(shape->head_dim, a, blocks, p.direct, st);
-    else if (layer->dtype == LA_BF16) e = rows_of_dim<__bf16, __bf16>(shape->head_dim, a, blocks, p.direct, st);
-    else e = rows_of_dim<__bf16, la::fp8_t>(shape->head_dim, a, blocks, p.direct, st);
-    if (e || p.direct) return e;
-    return join_rows(shape, a, rows, st);
+    if (layer->dtype == LA_F32) return decode_of_dim<float, float>(shape->head_dim, a, blocks, st);
+    if (layer->dtype == LA_BF16) return decode_of_dim<__bf16, __bf16>(shape->head_dim, a, blocks, st);
+    return decode_of_dim<__bf16, la::fp8_t>(shape->head_dim, a, blocks, st);
 }
 
 la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k, int64_t k_stride, const void *v, int64_t v_stride,

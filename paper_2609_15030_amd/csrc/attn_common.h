@@ -50,27 +50,25 @@ struct AttnArgs {
     const int32_t *prefix_len;     // decode: shared keys of each group
     float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
     int32_t n_seqs, kv_heads, group, n_groups;
-    int32_t max_kv;                // decode: longest kv_len the grid covers
-    int32_t part_tokens;           // decode: keys of one part (prefix; own keys: rows kernel)
+    int32_t max_kv;                // longest kv_len that the tables and the workspace cover
     int32_t parts;                 // parts the workspace holds for each row
-    int32_t group_tiles;           // decode: row tiles of the largest group
     int32_t prefix_parts;          // decode: of these, the most of a prefix
-    int32_t prefix_part_tokens;
+    int32_t group_tiles;           // decode: row tiles of the largest group
+    int32_t prefix_items;          // decode: workgroups of the prefixes, ahead of the others
+    bool split;                    // prompts: a workgroup for every part of the keys
+    bool direct;                   // decode: one part each, written straight to o
     float *part_o;                 // [row][parts][D]
     float2 *part_ml;               // [row][parts]
 };
 
-// --- the sizes of the parts of a prompt's keys ------------------------------
+// Keys of one part: prompts (also the steps in which an unsplit row joins its
+// sums, so that splitting changes no bit), shared prefixes, a sequence's own.
+constexpr int kPromptPart = 512;
+constexpr int kPrefixPart = 256;
+constexpr int kOwnPart = 256;
 
-// Keys per part of a sequence of `rows` rows under one key head that reads
-// `keys` keys (a multiple of 64; all keys: not split).
-__host__ __device__ inline int prompt_part_tokens(int64_t rows, int keys) {
-    return keys < 64 ? 64 : (keys + 63) & ~63;
-}
-
-__host__ __device__ inline int prompt_parts(int64_t rows, int keys) {
-    const int t = prompt_part_tokens(rows, keys);
-    return keys <= t ? 1 : (keys + t - 1) / t;
+__host__ __device__ inline int prompt_parts(bool split, int keys) {
+    return split && keys > kPromptPart ? (keys + kPromptPart - 1) / kPromptPart : 1;
 }
 
 // --- 16-byte pieces of rows, as the LDS tiles hold them ---------------------
@@ -128,30 +126,34 @@ template <typename T> __device__ inline bool drop_nonfinite(uint4 &x) {
     return any;
 }
 
-// Resource over `rows` keys or values (half 0 / 1) from token t on, for one key
-// head: rows at and past `hi` read as zero, as does a block that the table does
-// not name (counted).  The rows lie in one block.  Everything is wave-uniform.
-// HALF_BYTES: bytes of one head's row.
+// A block id read from the table for token t (0 past the last key): prefetched
+// ahead of the loads that use it.
+__device__ inline int block_of(const KvSource &s, const int32_t *table_row, int t, int hi) {
+    return t < hi ? table_row[t >> s.bt_shift] : 0;
+}
+
+// Keys and values of `rows` tokens from t on, which lie in one block, for one
+// key head, as buffer resources: rows at and past `hi` read as zero, as do those
+// of a block that the table does not name (counted).  All arguments are uniform.
+struct KvRows { __amdgpu_buffer_rsrc_t k, v; };
 template <bool PAGED>
-__device__ inline __amdgpu_buffer_rsrc_t kv_rows(const KvSource &s, int half, const int32_t *table_row, int64_t seq_row0,
-                                                 int kvh, int row_bytes, int t, int rows, int hi) {
-    const char *base = half ? s.v : s.k;
-    int n = hi - t;
-    n = n < 0 ? 0 : (n > rows ? rows : n);
+__device__ inline KvRows kv_rows(const KvSource &s, int id, int64_t seq_row0, int kvh, int row_bytes, int t, int rows, int hi) {
+    int n = min(hi - t, rows);
     if constexpr (PAGED) {
-        const int bt = 1 << s.bt_shift;
-        int id = n > 0 ? table_row[t >> s.bt_shift] : 0;
         if ((uint32_t)id >= (uint32_t)s.n_blocks) {
-            if (half == 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
+            if (n > 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
             id = 0;
             n = 0;
         }
-        const int64_t off = (int64_t)id * s.block_bytes + (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & (bt - 1)));
-        return make_rsrc(base + off, (uint32_t)(n * row_bytes));
+        const int64_t off = (int64_t)id * s.block_bytes +
+                            (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1)));
+        const uint32_t bytes = n > 0 ? (uint32_t)(n * row_bytes) : 0u;
+        return {make_rsrc(s.k + off, bytes), make_rsrc(s.v + off, bytes)};
     } else {
-        const int64_t stride = half ? s.v_stride : s.k_stride;
-        const char *p = base + (seq_row0 + t) * stride + (int64_t)kvh * row_bytes;
-        return make_rsrc(n > 0 ? p : base, n > 0 ? (uint32_t)((n - 1) * stride) + (uint32_t)row_bytes : 0u);
+        const int64_t row = n > 0 ? seq_row0 + t : 0, head = (int64_t)kvh * row_bytes;
+        const uint32_t kb = n > 0 ? (uint32_t)(n - 1) * (uint32_t)s.k_stride + (uint32_t)row_bytes : 0u;
+        const uint32_t vb = n > 0 ? (uint32_t)(n - 1) * (uint32_t)s.v_stride + (uint32_t)row_bytes : 0u;
+        return {make_rsrc(s.k + row * s.k_stride + head, kb), make_rsrc(s.v + row * s.v_stride + head, vb)};
     }
 }
 
@@ -180,6 +182,25 @@ __device__ inline bf16x8 join_tr(i16x4 a, i16x4 b) {
     const i16x8 x = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     return __builtin_bit_cast(bf16x8, x);
 }
+
+// (m, l, x) joined by the weight of a part's (mp, lp, xp): the running sums
+// shrink by *w, the part's by *wp.
+__device__ inline void join_weights(float &m, float &l, float mp, float lp, float *w, float *wp) {
+    const float m2 = fmaxf(m, mp), mu = m2 == -INFINITY ? 0.f : m2;
+    *w = __builtin_amdgcn_exp2f(m - mu);
+    *wp = __builtin_amdgcn_exp2f(mp - mu);
+    m = m2;
+    l = __builtin_fmaf(lp, *wp, l * *w);
+}
+__device__ inline f32x4 join4(f32x4 x, f32x4 xp, float w, float wp) {
+    f32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(xp[i], wp, x[i] * w);
+    return r;
+}
+
+// What a row's sums are multiplied by for its output.
+__device__ inline float row_scale(const AttnArgs &a, float l) { return l > 0.f || l != l ? a.v_scale / l : 0.f; }
 
 // Four consecutive outputs.
 __device__ inline void store4(float *p, f32x4 x) { *(f32x4 *)p = x; }

@@ -1,269 +1,362 @@
 // Attention of single tokens over a cache, and the joining of parts.
 //
-// attn_rows_kernel: a workgroup takes one part of the keys that a sequence has
-// to itself, for up to 16 query heads of one key head.  Every key and value is
-// used once by one wave, so nothing is shared: each of the eight waves takes
-// key tiles of its own, K goes from memory straight into the registers that the
-// product reads, V through LDS of the wave's own (its fragments are columns),
-// and the waves' m, l and sums meet at the end.
+// One launch holds two kinds of workgroups.  The first ones take the shared
+// prefixes, as tiles of rows (attn_tile.h).  The others take the keys that each
+// sequence has to itself, a part at a time, for up to 16 query heads of one key
+// head: every key and value is used once by one wave, so nothing is shared; each
+// of the eight waves takes key tiles of its own, K goes from memory straight into
+// the registers that the product reads, V through LDS of the wave's own (its
+// fragments are columns), and the waves' m, l and sums meet at the end.
 #pragma once
 #include "attn_tile.h"
 
 namespace la {
 
-constexpr int kRowsThreads = 512;
-constexpr int kRowsWaves = kRowsThreads / 64;
+constexpr int kDecodeWaves = 8;
+constexpr int kDecodeThreads8 = 64 * kDecodeWaves;
 constexpr int kRowsHeads = 16;
 
-// Keys of a wave's tile, and one tile of V in LDS (vpos as the row tiles').
-template <typename T, int D> struct RowsTile {
-    static constexpr int KT = sizeof(T) == 2 ? 32 : 16;
-    static constexpr int PPR = D / Piece<T>::N;
+template <typename T, int D> struct RowsLds {
+    static constexpr int KT = sizeof(T) == 2 ? 32 : 16;       // keys of a wave's tile
+    static constexpr int PS = AttnTile<T, D>::PS;
+    union {
+        uint4 v[kDecodeWaves][KT * PS];
+        float sum[kDecodeWaves][kRowsHeads][D];
+    };
+    float2 ml[kDecodeWaves][kRowsHeads];
 };
 
-// Own keys of sequence s of a decode call: [*first, *end); and the parts its prefix has.
-__device__ inline void own_keys(const AttnArgs &a, int s, bool count, int *first, int *end, int *prefix_parts) {
-    const int n = a.kv_len[s];
-    if (count && n > a.max_kv && a.kv.err) atomicAdd(a.kv.err, 1);
-    *end = max(0, min(n, a.max_kv));
+// Own keys [first, end) of sequence s of a decode call, and the parts of its
+// prefix.  Sequences outside every group share nothing.
+__device__ inline void own_keys(const AttnArgs &a, int s, int *first, int *end, int *prefix_parts) {
+    *end = max(0, min(a.kv_len[s], a.max_kv));
     *first = 0;
     *prefix_parts = 0;
     if (!a.cu_group) return;
-    const int lane = threadIdx.x & 63;
-    int g = 0;
-    for (int i0 = 0; i0 < a.n_groups; i0 += 64) {      // groups that begin at or before s
-        const int i = i0 + lane;
-        g += __popcll(__ballot(i < a.n_groups && a.cu_group[i] <= s));
+    int lo = 0, n = a.n_groups;                     // groups that begin at or before s
+    while (n > 0) {
+        const int half = n >> 1;
+        if (a.cu_group[lo + half] <= s) {
+            lo += half + 1;
+            n -= half + 1;
+        } else {
+            n = half;
+        }
     }
-    if (g == 0) return;
-    g = __builtin_amdgcn_readfirstlane(g - 1);
-    const int s1 = a.cu_group[g + 1];
+    if (lo == 0) return;
+    const int s1 = a.cu_group[lo];
     if (s >= s1) return;
-    const int shared = min(group_prefix(a, g, s1 - a.cu_group[g]), *end);
-    *first = shared;
-    *prefix_parts = (shared + a.prefix_part_tokens - 1) / a.prefix_part_tokens;
+    *first = min(group_prefix(a, lo - 1, s1 - a.cu_group[lo - 1]), *end);
+    *prefix_parts = (*first + kPrefixPart - 1) / kPrefixPart;
 }
 
 // Parts of own keys [first, end): they begin at the 16-token line at or before first.
-__device__ inline int own_parts(const AttnArgs &a, int first, int end) {
-    return end <= first ? 0 : (end - (first & ~15) + a.part_tokens - 1) / a.part_tokens;
+__device__ inline int own_parts(int first, int end) {
+    return end <= first ? 0 : (end - (first & ~15) + kOwnPart - 1) / kOwnPart;
 }
 
+// Workgroup b of n that take the own keys.
 template <typename T, typename C, int D>
-__global__ __launch_bounds__(kRowsThreads) void attn_rows_kernel(AttnArgs a, bool direct) {
-    using L = AttnTile<T, D>;
+__device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks, RowsLds<T, D> &sm) {
     using M = MT<T>;
-    constexpr int KT = RowsTile<T, D>::KT, PPR = RowsTile<T, D>::PPR, NT = KT / 16, DT = D / 16;
-    constexpr int NQ = sizeof(T) == 2 ? D / 32 : D / 16;
-    constexpr int RPL = 64 / PPR, VL = KT / RPL;               // V rows a load, loads of a tile
-    constexpr int RB = D * sizeof(C), CB = Piece<T>::N * sizeof(C);
-    constexpr int VBYTES = kRowsWaves * KT * PPR * 16, OBYTES = kRowsWaves * kRowsHeads * D * 4;
-    __shared__ uint4 smem[(VBYTES > OBYTES ? VBYTES : OBYTES) / 16];
-    __shared__ float2 wml[kRowsWaves][kRowsHeads];
+    using L = RowsLds<T, D>;
+    constexpr bool F8 = sizeof(C) == 1;
+    constexpr int KT = L::KT, PS = L::PS, NT = KT / 16, DT = D / 16;
+    constexpr int NQ = sizeof(T) == 2 ? D / 32 : D / 16;       // 16-byte pieces of a q row for each lane
+    constexpr int RB = D * sizeof(C);                          // bytes of a stored row
+    constexpr int NK = RB / 64, VPR = RB / 16, VR = 64 / VPR, VL = 16 / VR;    // loads of 16 keys, of 16 values
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    // key head fastest, then the row tiles of a wide group, the part, the sequence
-    uint32_t r = blockIdx.x;
-    const int kvh = (int)(r % (uint32_t)a.kv_heads);
-    r /= (uint32_t)a.kv_heads;
-    const int tiles = (a.group + kRowsHeads - 1) / kRowsHeads;
-    const int h0 = (int)(r % (uint32_t)tiles) * kRowsHeads;
-    r /= (uint32_t)tiles;
-    const int own_max = a.parts - a.prefix_parts;
-    const int part = (int)(r % (uint32_t)own_max), seq = (int)(r / (uint32_t)own_max);
-    int first, end, pp;
-    own_keys(a, seq, part == 0 && kvh == 0 && h0 == 0 && threadIdx.x == 0, &first, &end, &pp);
-    const int lo = (first & ~15) + part * a.part_tokens;
-    const int hi = min(end, lo + a.part_tokens);
-    if (lo >= hi && !(direct && part == 0)) return;
-    const bool live = h0 + col < a.group;
-    const int head = kvh * a.group + h0 + (live ? col : 0);
-    const int32_t *table_row = a.kv.table + (int64_t)seq * a.kv.max_blocks;
-
-    uint4 qf[NQ];
-    {
-        const T *qp = (const T *)a.q + seq * a.q_stride + (int64_t)head * D;
+    const int tiles = (a.group + kRowsHeads - 1) / kRowsHeads, heads = tiles * a.kv_heads;
+    // the call's items (part of a sequence, key head, row tile; the last fastest), and this workgroup's share
+    auto parts_of = [&](int i) {
+        int first, end, pp;
+        own_keys(a, i, &first, &end, &pp);
+        const int n = own_parts(first, end);
+        return a.direct && n == 0 ? 1 : n;
+    };
+    int total = 0;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        int x = i0 + lane < a.n_seqs ? parts_of(i0 + lane) : 0;
 #pragma unroll
-        for (int s = 0; s < NQ; ++s) qf[s] = live ? *(const uint4 *)(qp + (4 * s + g) * Piece<T>::N) : make_uint4(0, 0, 0, 0);
+        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+        total += x;
     }
-    f32x4 acc[DT];
+    total = __builtin_amdgcn_readfirstlane(total) * heads;
+    const int per = total / n_blocks, extra = total - per * n_blocks;
+    int item = b * per + min(b, extra);
+    const int stop = item + per + (b < extra);
+    if (b == 0 && a.kv.err)
+        for (int i = threadIdx.x; i < a.n_seqs; i += kDecodeThreads8)
+            if (a.kv_len[i] > a.max_kv) atomicAdd(a.kv.err, 1);
+    if (item >= stop) return;
+    int seq, part;
+    if (!item_of(a.n_seqs, item / heads, parts_of, &seq, &part)) return;
+    int at = item % heads;
+    int first, end, pp;
+    own_keys(a, seq, &first, &end, &pp);
+
+    for (; item < stop; ++item) {
+        const int kvh = at / tiles, h0 = (at - kvh * tiles) * kRowsHeads;
+        const int lo = (first & ~15) + part * kOwnPart;
+        const int hi = min(end, lo + kOwnPart);
+        const int live_heads = min(kRowsHeads, a.group - h0);
+        const bool live = col < live_heads;
+        const int head = kvh * a.group + h0 + (live ? col : 0);
+        // block ids of the part's runs of 16 keys, one a lane
+        static_assert(kOwnPart / 16 <= 64, "a lane for each run of 16 keys");
+        const int ids = block_of(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo + 16 * (lane & (kOwnPart / 16 - 1)), hi);
+        uint4 qf[NQ];
+        {
+            const T *qp = (const T *)a.q + seq * a.q_stride + (int64_t)head * D;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] = zero4();
-    float m = -INFINITY, l = 0.f;
-    uint4 *vt = smem + wave * KT * PPR;
-    for (int t0 = lo + wave * KT; t0 < hi; t0 += kRowsWaves * KT) {
-        Raw<C> kr[NT][NQ], vr[VL];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const auto res = kv_rows<true>(a.kv, 0, table_row, 0, kvh, RB, t0 + 16 * n, 16, hi);
-#pragma unroll
-            for (int k = 0; k < NQ; ++k) kr[n][k] = load_piece<C>(res, (uint32_t)(col * RB + (4 * k + g) * CB));
+            for (int s = 0; s < NQ; ++s) {
+                // an 8-bit key load holds 16 dims of a lane: the pieces of two products
+                const int p = F8 ? 8 * (s >> 1) + 2 * g + (s & 1) : 4 * s + g;
+                qf[s] = live ? *(const uint4 *)(qp + p * Piece<T>::N) : make_uint4(0, 0, 0, 0);
+            }
         }
+        f32x4 acc[DT];
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const auto res = kv_rows<true>(a.kv, 1, table_row, 0, kvh, RB, t0 + RPL * i, RPL, hi);
-            vr[i] = load_piece<C>(res, (uint32_t)((lane / PPR) * RB + (lane % PPR) * CB));
-        }
-        f32x4 s[NT];
+        for (int d = 0; d < DT; ++d) acc[d] = zero4();
+        float m = -INFINITY, l = 0.f;
+        char *const vt = (char *)sm.v[wave];
+        for (int t0 = lo + wave * KT; t0 < hi; t0 += kDecodeWaves * KT) {
+            uint4 kr[NT][NK], vr[NT][VL];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            s[n] = zero4();
+            for (int n = 0; n < NT; ++n) {
+                const int id = __builtin_amdgcn_readlane(ids, (t0 - lo) / 16 + n);
+                const auto res = kv_rows<true>(a.kv, id, 0, kvh, RB, t0 + 16 * n, 16, hi);
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) {
-                const uint4 kf = piece_of<C>(kr[n][k]);
-                if constexpr (sizeof(T) == 2) {
-                    s[n] = M::mma(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), s[n]);
-                } else {
-                    const float *x = (const float *)&kf, *y = (const float *)&qf[k];
+                for (int k = 0; k < NK; ++k) kr[n][k] = buf_load16(res.k, (uint32_t)(col * RB + 16 * g), 64 * k);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[n] = M::mma(x[e], y[e], s[n]);
+                for (int i = 0; i < VL; ++i) vr[n][i] = buf_load16(res.v, (uint32_t)(16 * lane), 1024 * i);
+            }
+            f32x4 s[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n] = zero4();
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    const uint4 x = kr[n][k];
+                    if constexpr (F8) {
+                        const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
+                        s[n] = M::mma(__builtin_bit_cast(bf16x8, make_uint4(e0.x, e0.y, e1.x, e1.y)),
+                                      __builtin_bit_cast(bf16x8, qf[2 * k]), s[n]);
+                        s[n] = M::mma(__builtin_bit_cast(bf16x8, make_uint4(e2.x, e2.y, e3.x, e3.y)),
+                                      __builtin_bit_cast(bf16x8, qf[2 * k + 1]), s[n]);
+                    } else if constexpr (sizeof(T) == 2) {
+                        s[n] = M::mma(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, qf[k]), s[n]);
+                    } else {
+                        const float *e = (const float *)&x, *y = (const float *)&qf[k];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[n] = M::mma(e[j], y[j], s[n]);
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < VL; ++i) vt[L::vpos(RPL * i + lane / PPR, lane % PPR)] = piece_of<C>(vr[i]);
-        const bool masked = t0 < first || t0 + KT > hi;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < VL; ++i) {
+                    uint4 *const to = (uint4 *)vt + (16 * n + VR * i + lane / VPR) * PS;
+                    const uint4 x = vr[n][i];
+                    if constexpr (F8) {
+                        const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
+                        to[2 * (lane % VPR)] = make_uint4(e0.x, e0.y, e1.x, e1.y);
+                        to[2 * (lane % VPR) + 1] = make_uint4(e2.x, e2.y, e3.x, e3.y);
+                    } else {
+                        to[lane % VPR] = x;
+                    }
+                }
+            const bool masked = t0 < first || t0 + KT > hi;
+            float top = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = s[n][i] * a.c;
+                    const int tok = t0 + 16 * n + 4 * g + i;
+                    if (masked && (tok < first || tok >= hi)) x = -INFINITY;
+                    s[n][i] = x;
+                    top = fmaxf(top, x);
+                }
+            const float m2 = fmaxf(m, row_max16(top));
+            const float mu = m2 == -INFINITY ? 0.f : m2;
+            const float shrink = __builtin_amdgcn_exp2f(m - mu);
+            m = m2;
+            l *= shrink;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - mu);
+                    l += s[n][i];
+                }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[d][i] *= shrink;
+            if constexpr (sizeof(T) == 2) {
+                const bf16x8 p = pack8(s[0], s[1]);
+                const char *x = vt + (4 * g + (col >> 2)) * PS * 16 + 8 * (col & 3);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d] = M::mma(join_tr(lds_tr(x + 32 * d), lds_tr(x + 16 * PS * 16 + 32 * d)), p, acc[d]);
+            } else {
+                const char *x = vt + 4 * g * PS * 16 + 4 * col;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) acc[d] = M::mma(*(const float *)(x + i * PS * 16 + 64 * d), s[0][i], acc[d]);
+            }
+        }
+        // the waves' results: every wave scales its sums to the common maximum
+        l = row_sum16(l);
+        if (g == 0) sm.ml[wave][col] = make_float2(m, l);
+        __syncthreads();
         float top = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, sm.ml[w][col].x);
+        const float scale = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+        if (live) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x = s[n][i] * a.c;
-                const int tok = t0 + 16 * n + 4 * g + i;
-                if (masked && (tok < first || tok >= hi)) x = -INFINITY;
-                s[n][i] = x;
-                top = fmaxf(top, x);
-            }
-        const float m2 = fmaxf(m, row_max16(top));
-        const float mu = m2 == -INFINITY ? 0.f : m2;
-        const float shrink = __builtin_amdgcn_exp2f(m - mu);
-        m = m2;
-        l *= shrink;
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - mu);
-                l += s[n][i];
-            }
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[d][i] *= shrink;
-        const char *vb = (const char *)vt;
-        if constexpr (sizeof(T) == 2) {
-            const bf16x8 p = pack8(s[0], s[1]);
-            const int vr0 = 4 * g + (col >> 2);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const int pc = 2 * d + ((col & 3) >> 1), half = 8 * (col & 1);
-                acc[d] = M::mma(join_tr(lds_tr(vb + L::vpos(vr0, pc) * 16 + half), lds_tr(vb + L::vpos(vr0 + 16, pc) * 16 + half)),
-                                p, acc[d]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    acc[d] = M::mma(*(const float *)(vb + L::vpos(4 * g + i, 4 * d + (col >> 2)) * 16 + 4 * (col & 3)), s[0][i],
-                                    acc[d]);
+            for (int d = 0; d < DT; ++d) *(f32x4 *)&sm.sum[wave][col][16 * d + 4 * g] = acc[d] * scale;
         }
-    }
-    // the waves' results: every wave scales its sums to the common maximum
-    l = row_sum16(l);
-    if (g == 0) wml[wave][col] = make_float2(m, l);
-    __syncthreads();
-    float top = -INFINITY;
+        __syncthreads();
+        for (int e = threadIdx.x; e < live_heads * (D / 4); e += kDecodeThreads8) {
+            const int h = e / (D / 4), d = e % (D / 4) * 4;
+            f32x4 x = zero4();
+            float lt = 0.f, mt = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kRowsWaves; ++w) top = fmaxf(top, wml[w][col].x);
-    const float mu = top == -INFINITY ? 0.f : top;
-    const float scale = __builtin_amdgcn_exp2f(m - mu);
-    float *so = (float *)smem;                                  // [wave][head][D], V no longer needed
+            for (int w = 0; w < kDecodeWaves; ++w) mt = fmaxf(mt, sm.ml[w][h].x);
+            const float mh = mt == -INFINITY ? 0.f : mt;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *(f32x4 *)&so[(wave * kRowsHeads + col) * D + 16 * d + 4 * g] = acc[d] * scale;
-    __syncthreads();
-    for (int e = threadIdx.x; e < kRowsHeads * D / 4; e += kRowsThreads) {
-        const int h = e / (D / 4), d = e % (D / 4) * 4;
-        if (h0 + h >= a.group) continue;
-        f32x4 x = zero4();
-        float lt = 0.f, mt = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) mt = fmaxf(mt, wml[w][h].x);
-        const float mh = mt == -INFINITY ? 0.f : mt;
-#pragma unroll
-        for (int w = 0; w < kRowsWaves; ++w) {
-            x += *(const f32x4 *)&so[(w * kRowsHeads + h) * D + d];
-            lt += wml[w][h].y * __builtin_amdgcn_exp2f(wml[w][h].x - mh);
+            for (int w = 0; w < kDecodeWaves; ++w) {
+                x += *(const f32x4 *)&sm.sum[w][h][d];
+                lt += sm.ml[w][h].y * __builtin_amdgcn_exp2f(sm.ml[w][h].x - mh);
+            }
+            const int64_t head_row = (int64_t)kvh * a.group + h0 + h;
+            if (a.direct) {
+                store4((T *)a.o + seq * a.o_stride + head_row * D + d, x * row_scale(a, lt));
+            } else {
+                const int64_t slot = ((int64_t)seq * a.kv_heads * a.group + head_row) * a.parts + pp + part;
+                store4(a.part_o + slot * D + d, x);
+                if (d == 0) a.part_ml[slot] = make_float2(mt, lt);
+            }
         }
-        const int64_t row = (int64_t)seq * a.kv_heads * a.group + kvh * a.group + h0 + h;
-        if (direct) {
-            const float inv = lt > 0.f || lt != lt ? a.v_scale / lt : 0.f;
-            store4((T *)a.o + seq * a.o_stride + (int64_t)(kvh * a.group + h0 + h) * D + d, x * inv);
-        } else {
-            const int64_t slot = row * a.parts + pp + part;
-            store4(a.part_o + slot * D + d, x);
-            if (d == 0) a.part_ml[slot] = make_float2(mt, lt);
+        // the next item: the next head, part or sequence that has one
+        if (++at == heads && item + 1 < stop) {
+            at = 0;
+            if (++part >= own_parts(first, end)) {
+                part = 0;
+                do {
+                    ++seq;
+                    own_keys(a, seq, &first, &end, &pp);
+                } while (!a.direct && own_parts(first, end) == 0);
+            }
         }
+        __syncthreads();                                        // sums read before the next item's V lands there
     }
 }
 
-// Joins the parts of every row that has them: a wave a row.  Lane p holds part
-// p's weight (64 parts a step); D / 64 sums each.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int64_t n_rows) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (row >= n_rows) return;
-    const int heads = a.kv_heads * a.group;
-    const int64_t tok = row / heads;
-    const int head = (int)(row - tok * heads);
-    int n;
-    if (a.cu) {
-        int seq, local;
-        if (!item_of(a.n_seqs, (int)tok, [&](int i) { return a.cu[i + 1] - a.cu[i]; }, &seq, &local)) return;
-        const int new_tokens = a.cu[seq + 1] - a.cu[seq], rows = new_tokens * a.group, keys = prompt_keys(a, seq);
-        if (prompt_parts(rows, keys) == 1) return;             // written by its tile
-        const int limit = max(0, min(keys, keys - new_tokens + local + 1)), pt = prompt_part_tokens(rows, keys);
-        n = (limit + pt - 1) / pt;
+template <typename T, typename C, int D>
+__global__ __launch_bounds__(kDecodeThreads8, sizeof(T) == 2 ? 4 : 2) void attn_decode_kernel(AttnArgs a) {
+    __shared__ union Lds {
+        TileLds<T, D, kDecodeWaves> tile;
+        RowsLds<T, D> rows;
+    } sm;
+    if ((int)blockIdx.x < a.prefix_items) {
+        RowTile t;
+        if (prefix_tile_of<16 * kDecodeWaves>(a, blockIdx.x, &t)) tile_run<T, C, D, true, kDecodeWaves>(a, t, sm.tile);
     } else {
-        int first, end, pp;
-        own_keys(a, (int)tok, false, &first, &end, &pp);
-        n = pp + own_parts(a, first, end);
+        rows_run<T, C, D>(a, (int)blockIdx.x - a.prefix_items, (int)gridDim.x - a.prefix_items, sm.rows);
     }
-    const float2 *ml = a.part_ml + row * a.parts;
-    const float *po = a.part_o + row * a.parts * D;
-    float m = -INFINITY, l = 0.f, x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.f;
-    for (int p0 = 0; p0 < n; p0 += 64) {
-        const float2 y = p0 + lane < n ? ml[p0 + lane] : make_float2(-INFINITY, 0.f);
-        float top = y.x;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-        const float m2 = fmaxf(m, top), mu = m2 == -INFINITY ? 0.f : m2;
-        const float shrink = __builtin_amdgcn_exp2f(m - mu);
-        const float w = __builtin_amdgcn_exp2f(y.x - mu);
-        m = m2;
-        l *= shrink;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] *= shrink;
-        l += w * y.y;                                            // this lane's part
-        const int most = min(64, n - p0);
-        for (int p = 0; p < most; ++p) {
-            const float wp = __shfl(w, p);
-            const float *src = po + (int64_t)(p0 + p) * D + lane * E;
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[e] += wp * src[e];
+}
+
+// Joins the parts of prompt rows, in the order and by the sums in which an
+// unsplit tile joins them.  D / 4 lanes a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a, int64_t n_rows) {
+    constexpr int LANES = D / 4, AHEAD = 4;
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int heads = a.kv_heads * a.group;
+    const int64_t tok = min(row, n_rows - 1) / heads;
+    const int head = (int)(row - tok * heads);
+    int lo = 0, n = a.n_seqs;                        // the last sequence that begins at or before the token
+    while (n > 1) {
+        const int half = n >> 1;
+        if (a.cu[lo + half] <= tok) {
+            lo += half;
+            n -= half;
+        } else {
+            n = half;
         }
     }
+    if (row >= n_rows) return;
+    const int new_tokens = a.cu[lo + 1] - a.cu[lo], keys = prompt_keys(a, lo);
+    if (prompt_parts(a.split, keys) == 1) return;                // written by its tile
+    const int limit = max(0, keys - new_tokens + (int)(tok - a.cu[lo]) + 1);
+    const int parts = (limit + kPromptPart - 1) / kPromptPart;
+    const float2 *ml = a.part_ml + row * a.parts;
+    const float *po = a.part_o + row * a.parts * D + 4 * lane;
+    float m = -INFINITY, l = 0.f;
+    f32x4 x = zero4();
+    for (int p0 = 0; p0 < parts; p0 += AHEAD) {
+        f32x4 xp[AHEAD];
+        float2 y[AHEAD];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-    const float inv = l > 0.f || l != l ? a.v_scale / l : 0.f;
-    T *op = (T *)a.o + tok * a.o_stride + (int64_t)head * D + lane * E;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int p = min(p0 + i, parts - 1);
+            xp[i] = *(const f32x4 *)(po + (int64_t)p * D);
+            y[i] = ml[p];
+        }
 #pragma unroll
-    for (int e = 0; e < E; ++e) op[e] = from_f32<T>(x[e] * inv);
+        for (int i = 0; i < AHEAD; ++i) {
+            if (p0 + i >= parts) break;
+            float w, wp;
+            join_weights(m, l, y[i].x, y[i].y, &w, &wp);
+            x = join4(x, xp[i], w, wp);
+        }
+    }
+    store4((T *)a.o + tok * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
+}
+
+// Joins the parts of a single token's row: a workgroup a row, D / 4 lanes a part.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+    constexpr int LANES = D / 4, SETS = 256 / LANES;
+    __shared__ f32x4 xs[SETS][LANES];
+    __shared__ float2 mls[SETS];
+    const int set = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const int heads = a.kv_heads * a.group;
+    const uint32_t row = blockIdx.x, seq = row / (uint32_t)heads, head = row - seq * (uint32_t)heads;
+    int first, end, pp;
+    own_keys(a, (int)seq, &first, &end, &pp);
+    const int parts = pp + own_parts(first, end);
+    const float2 *ml = a.part_ml + (int64_t)row * a.parts;
+    const float *po = a.part_o + (int64_t)row * a.parts * D + 4 * lane;
+    float m = -INFINITY, l = 0.f;
+    f32x4 x = zero4();
+#pragma unroll 4
+    for (int p = set; p < parts; p += SETS) {
+        const float2 y = ml[p];
+        const f32x4 xp = *(const f32x4 *)(po + (int64_t)p * D);
+        float w, wp;
+        join_weights(m, l, y.x, y.y, &w, &wp);
+        x = join4(x, xp, w, wp);
+    }
+    xs[set][lane] = x;
+    if (lane == 0) mls[set] = make_float2(m, l);
+    __syncthreads();
+    if (set > 0) return;
+#pragma unroll
+    for (int i = 1; i < SETS; ++i) {
+        float w, wp;
+        join_weights(m, l, mls[i].x, mls[i].y, &w, &wp);
+        x = join4(x, xs[i][lane], w, wp);
+    }
+    store4((T *)a.o + (int64_t)seq * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
 }
 
 }  // namespace la

@@ -1,32 +1,26 @@
-// Attention of tiles of 64 rows, 16 for each of four waves, over key tiles in
-// LDS: prompts of few rows, fp32 prompts, and the shared prefix of a decode
-// group (rows: the group's sequences; every row reads the same keys).
+// Attention of tiles of rows, 16 for each wave, over key tiles in LDS: prompts of
+// few rows, fp32 prompts, and the shared prefix of a decode group (rows: the
+// group's sequences; every row reads the same keys).
+//
+// Key tiles are double buffered, and two more are in flight in registers, so that
+// a tile's loads have two tiles' time to arrive: a workgroup's tile takes about a
+// microsecond and memory about as long to answer.
 #pragma once
 #include "attn_common.h"
 
 namespace la {
 
-constexpr int kTileThreads = 256;
-constexpr int kTileRows = 64;
-
-// Key tile of the kernel and the layout of one tile in LDS: rows of 16-byte
-// pieces.  kpos: 16 rows of one piece (a K fragment) fall on 16 different pieces
-// of the 64 banks; vpos: so do the 16 rows x 32 bytes (bf16) or 4 rows x 64
-// bytes (fp32) that a V fragment reads at once.
+// Key tile of the kernel and one tile of rows in LDS: 16-byte pieces, one piece of
+// padding behind each row.  With it the 16 rows of one piece (a K fragment) fall
+// on different banks, the 16 rows x 32 bytes (bf16) that a V fragment's transposed
+// reads take at once on every bank twice, and the 4 rows x 64 bytes (fp32) on
+// different banks; and a lane's addresses differ by constants, which an
+// exclusive-or of row and piece would not give (it took 40 more registers).
 template <typename T, int D> struct AttnTile {
-    static constexpr int N = Piece<T>::N, PPR = D / N;
+    static constexpr int N = Piece<T>::N, PPR = D / N, PS = PPR + 1;
     static constexpr int KT = sizeof(T) == 2 || D == 64 ? 64 : 32;
     static constexpr int RPL = 64 / PPR;                  // rows that a wave loads at once
-    static constexpr int LOADS = KT / (4 * RPL);
-    __device__ static inline int kpos(int row, int p) {
-        if constexpr (PPR == 8) return row * PPR + (p ^ ((row >> 1) & 7));
-        else return row * PPR + (p ^ (row & 15));
-    }
-    __device__ static inline int vpos(int row, int p) {
-        if constexpr (sizeof(T) == 4) return row * PPR + (p ^ (((row >> 2) & 3) << 2));
-        else if constexpr (PPR == 8) return row * PPR + (p ^ (((row >> 1) & 3) << 1));
-        else return row * PPR + (p ^ ((row & 7) << 1));
-    }
+    static constexpr int PIECES = KT * PS;
 };
 
 // The tile of rows that a workgroup works on (all values uniform).
@@ -45,14 +39,14 @@ struct RowTile {
 __device__ inline int row_limit(const AttnArgs &a, const RowTile &t, int row) {
     if (row >= t.n_rows) return 0;
     const int tok = row / a.group;
-    if (t.prefix) return min(t.keys, min(a.kv_len[t.tok0 + tok], a.max_kv));
+    if (t.prefix) return max(0, min(t.keys, min(a.kv_len[t.tok0 + tok], a.max_kv)));
     return max(0, min(t.keys, t.pos0 + tok + 1));
 }
 
 // Shared keys of a group: none if it has only one member (its keys are then all its own).
 __device__ inline int group_prefix(const AttnArgs &a, int g, int members) {
     if (members < 2) return 0;
-    return max(0, min(a.prefix_len[g], a.prefix_parts * a.prefix_part_tokens));
+    return max(0, min(a.prefix_len[g], a.prefix_parts * kPrefixPart));
 }
 
 // Keys of sequence i of a prompt call.
@@ -60,36 +54,40 @@ __device__ inline int prompt_keys(const AttnArgs &a, int i) {
     return a.kv_len ? max(0, min(a.kv_len[i], a.max_kv)) : a.cu[i + 1] - a.cu[i];
 }
 
-// The work of block `b`; false: none.  The key head is the fastest index, so that
-// the heads of one row tile run side by side and, with 8 heads or a divisor of 8,
-// an XCD (workgroup id mod 8) keeps to one head's keys.  A prompt's longest
-// (last) tiles come first.
+// The work of item `b` of a call; false: none.  The key head is the fastest
+// index, so that the heads of one row tile run side by side and, with 8 heads or
+// a divisor of 8, an XCD (workgroup id mod 8) keeps to one head's keys.  A
+// prompt's longest (last) tiles come first.
 template <int ROWS>
-__device__ inline bool row_tile_of(const AttnArgs &a, RowTile *t) {
-    const uint32_t b = blockIdx.x;
+__device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t) {
+    int r = (int)(b / (uint32_t)a.kv_heads);
+    t->kvh = (int)(b - (uint32_t)r * (uint32_t)a.kv_heads);
+    t->prefix = true;
+    const int tile = r % a.group_tiles;
+    r /= a.group_tiles;
+    t->part = r % a.prefix_parts;
+    const int g = r / a.prefix_parts;
+    const int s0 = a.cu_group[g], members = a.cu_group[g + 1] - s0;
+    t->seq = s0;
+    t->tok0 = s0;
+    t->n_rows = members * a.group;
+    t->row0 = tile * ROWS;
+    t->pos0 = 0;
+    t->keys = group_prefix(a, g, members);
+    t->n_parts = 2;
+    t->lo = t->part * kPrefixPart;
+    t->hi = min(t->keys, t->lo + kPrefixPart);
+    return t->row0 < t->n_rows && t->lo < t->hi;
+}
+
+template <int ROWS>
+__device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t) {
     const int r = (int)(b / (uint32_t)a.kv_heads);
     t->kvh = (int)(b - (uint32_t)r * (uint32_t)a.kv_heads);
-    t->prefix = a.cu_group != nullptr;
-    if (t->prefix) {
-        const int tile = r % a.group_tiles, q = r / a.group_tiles;
-        t->part = q % a.prefix_parts;
-        const int g = q / a.prefix_parts;
-        if (g >= a.n_groups) return false;
-        const int s0 = a.cu_group[g], members = a.cu_group[g + 1] - s0;
-        t->seq = s0;
-        t->tok0 = s0;
-        t->n_rows = members * a.group;
-        t->row0 = tile * ROWS;
-        t->pos0 = 0;
-        t->keys = group_prefix(a, g, members);
-        t->n_parts = 2;
-        t->lo = t->part * a.prefix_part_tokens;
-        t->hi = min(t->keys, t->lo + a.prefix_part_tokens);
-        return t->row0 < t->n_rows && t->lo < t->hi;
-    }
+    t->prefix = false;
     auto items = [&](int i) {
         const int rows = (a.cu[i + 1] - a.cu[i]) * a.group;
-        return (rows + ROWS - 1) / ROWS * prompt_parts(rows, prompt_keys(a, i));
+        return (rows + ROWS - 1) / ROWS * prompt_parts(a.split, prompt_keys(a, i));
     };
     int seq, local;
     if (!item_of(a.n_seqs, r, items, &seq, &local)) return false;
@@ -99,18 +97,16 @@ __device__ inline bool row_tile_of(const AttnArgs &a, RowTile *t) {
     t->keys = prompt_keys(a, seq);
     const int tiles = (rows + ROWS - 1) / ROWS;
     t->n_rows = rows;
-    t->n_parts = prompt_parts(rows, t->keys);
+    t->n_parts = prompt_parts(a.split, t->keys);
     t->part = local / tiles;
     t->row0 = (tiles - 1 - local % tiles) * ROWS;
     t->pos0 = t->keys - rows / a.group;
-    t->prefix = false;
     t->hi = row_limit(a, *t, min(t->row0 + ROWS, t->n_rows) - 1);
     t->lo = 0;
     if (t->n_parts > 1) {
-        const int pt = prompt_part_tokens(rows, t->keys);
-        t->lo = t->part * pt;
-        t->hi = min(t->hi, t->lo + pt);
-        return t->lo < t->hi || (t->part == 0);
+        t->lo = t->part * kPromptPart;
+        t->hi = min(t->hi, t->lo + kPromptPart);
+        return t->lo < t->hi;
     }
     return true;
 }
@@ -152,19 +148,21 @@ __device__ inline void add_nonfinite(const AttnArgs &a, const int32_t *table_row
     }
 }
 
-template <typename T, typename C, int D, bool PAGED>
-__global__ __launch_bounds__(kTileThreads) void attn_tile_kernel(AttnArgs a) {
+// LDS of a workgroup of NW waves.
+template <typename T, int D, int NW> struct TileLds {
+    uint4 k[2][AttnTile<T, D>::PIECES], v[2][AttnTile<T, D>::PIECES];
+    int least[NW], dropped;
+};
+
+template <typename T, typename C, int D, bool PAGED, int NW>
+__device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, TileLds<T, D, NW> &sm) {
     using L = AttnTile<T, D>;
     using M = MT<T>;
-    constexpr int KT = L::KT, NT = KT / 16, DT = D / 16;
+    constexpr int KT = L::KT, NT = KT / 16, DT = D / 16, LOADS = KT / (NW * L::RPL);
     constexpr int NQ = sizeof(T) == 2 ? D / 32 : D / 16;       // 16-byte pieces of a q row for each lane
-    constexpr int CB = Piece<T>::N * sizeof(C);                // stored bytes of one piece
-    __shared__ uint4 kbuf[2][KT * L::PPR];
-    __shared__ uint4 vbuf[2][KT * L::PPR];
-    __shared__ int least[4], dropped;
+    constexpr int CB = Piece<T>::N * sizeof(C), RB = D * sizeof(C);    // stored bytes of a piece, of a row
+    static_assert(LOADS >= 1 && LOADS * NW * L::RPL == KT && kPromptPart % (2 * KT) == 0, "key tile");
 
-    RowTile t;
-    if (!row_tile_of<kTileRows>(a, &t)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int row = t.row0 + 16 * wave + col;
@@ -174,6 +172,33 @@ __global__ __launch_bounds__(kTileThreads) void attn_tile_kernel(AttnArgs a) {
     const int head = t.kvh * a.group + (live ? row % a.group : 0);
     const int32_t *table_row = PAGED ? a.kv.table + (int64_t)t.seq * a.kv.max_blocks : nullptr;
     const int64_t seq_row0 = PAGED ? 0 : t.tok0;
+    const int lrow = lane / L::PPR, lp = lane % L::PPR;
+    const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
+    const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
+
+    // Tile x's loads: rows (NW i + wave) RPL + lrow of it.  The block ids of the
+    // tile after it are read from the table meanwhile.
+    int ids[LOADS];
+    auto look = [&](int t0) {
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) ids[i] = block_of(a.kv, table_row, t0 + (NW * i + wave) * L::RPL, t.hi);
+        }
+    };
+    struct Flight { Raw<C> k[LOADS], v[LOADS]; };
+    auto load = [&](int t0, Flight &f) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const auto res = kv_rows<PAGED>(a.kv, PAGED ? ids[i] : 0, seq_row0, t.kvh, RB, t0 + (NW * i + wave) * L::RPL, L::RPL, t.hi);
+            f.k[i] = load_piece<C>(res.k, kvoff);
+            f.v[i] = load_piece<C>(res.v, vvoff);
+        }
+        look(t0 + KT);
+    };
+    look(t.lo);
+    Flight f0, f1;
+    load(t.lo, f0);
+    load(t.lo + KT, f1);
 
     uint4 qf[NQ];
     {
@@ -189,147 +214,167 @@ __global__ __launch_bounds__(kTileThreads) void attn_tile_kernel(AttnArgs a) {
         int lo = live ? limit : 0x7fffffff;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) lo = min(lo, __shfl_xor(lo, d));
-        if (lane == 0) least[wave] = lo;
-        if (threadIdx.x == 0) dropped = 0;
+        if (lane == 0) sm.least[wave] = lo;
+        if (threadIdx.x == 0) sm.dropped = 0;
     }
     int wave_hi = limit;
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) wave_hi = max(wave_hi, __shfl_xor(wave_hi, d));
     wave_hi = __builtin_amdgcn_readfirstlane(min(wave_hi, t.hi));
     __syncthreads();
-    const int all_see = __builtin_amdgcn_readfirstlane(min(min(least[0], least[1]), min(least[2], least[3])));
-
-    Raw<C> kr[L::LOADS], vr[L::LOADS];
-    const int lrow = lane / L::PPR, lp = lane % L::PPR;
-    auto load = [&](int t0) {
+    int all_see = sm.least[0];
 #pragma unroll
-        for (int i = 0; i < L::LOADS; ++i) {
-            const int r = (4 * i + wave) * L::RPL;
-            const auto kres = kv_rows<PAGED>(a.kv, 0, table_row, seq_row0, t.kvh, D * (int)sizeof(C), t0 + r, L::RPL, t.hi);
-            const auto vres = kv_rows<PAGED>(a.kv, 1, table_row, seq_row0, t.kvh, D * (int)sizeof(C), t0 + r, L::RPL, t.hi);
-            const int ks = PAGED ? D * (int)sizeof(C) : (int)a.kv.k_stride, vs = PAGED ? D * (int)sizeof(C) : (int)a.kv.v_stride;
-            kr[i] = load_piece<C>(kres, (uint32_t)(lrow * ks + lp * CB));
-            vr[i] = load_piece<C>(vres, (uint32_t)(lrow * vs + lp * CB));
-        }
-    };
-    auto store = [&](int b, int t0) {
+    for (int w = 1; w < NW; ++w) all_see = min(all_see, sm.least[w]);
+    all_see = __builtin_amdgcn_readfirstlane(all_see);
+
+    auto store = [&](int b, int t0, const Flight &f) {
         const bool mixed = t0 + KT > all_see;
 #pragma unroll
-        for (int i = 0; i < L::LOADS; ++i) {
-            const int r = (4 * i + wave) * L::RPL + lrow;
-            kbuf[b][L::kpos(r, lp)] = piece_of<C>(kr[i]);
-            uint4 v = piece_of<C>(vr[i]);
-            if (mixed && drop_nonfinite<T>(v)) dropped = 1;
-            vbuf[b][L::vpos(r, lp)] = v;
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = ((NW * i + wave) * L::RPL + lrow) * L::PS + lp;
+            sm.k[b][at] = piece_of<C>(f.k[i]);
+            uint4 v = piece_of<C>(f.v[i]);
+            if (mixed && drop_nonfinite<T>(v)) sm.dropped = 1;
+            sm.v[b][at] = v;
         }
     };
 
-    f32x4 acc[DT];
+    f32x4 acc[DT], sum[DT];
 #pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] = zero4();
-    float m = -INFINITY, l = 0.f;
-    if (t.lo < t.hi) {
-        load(t.lo);
-        store(0, t.lo);
-    }
-    __syncthreads();
-    int b = 0;
-    for (int t0 = t.lo; t0 < t.hi; t0 += KT, b ^= 1) {
-        const bool more = t0 + KT < t.hi;
-        if (more) load(t0 + KT);
-        if (t0 < wave_hi) {
-            f32x4 s[NT];
+    for (int i = 0; i < DT; ++i) acc[i] = sum[i] = zero4();
+    float m = -INFINITY, l = 0.f, sum_m = -INFINITY, sum_l = 0.f;
+    auto compute = [&](int b, int t0) {
+        if (t0 >= wave_hi) return;
+        f32x4 s[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s[n] = zero4();
+        for (int n = 0; n < NT; ++n) {
+            s[n] = zero4();
 #pragma unroll
-                for (int k = 0; k < NQ; ++k) {
-                    const uint4 kf = kbuf[b][L::kpos(16 * n + col, 4 * k + g)];
-                    if constexpr (sizeof(T) == 2) {
-                        s[n] = M::mma(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), s[n]);
-                    } else {
-                        const float *x = (const float *)&kf, *y = (const float *)&qf[k];
+            for (int k = 0; k < NQ; ++k) {
+                const uint4 kf = sm.k[b][(16 * n + col) * L::PS + 4 * k + g];
+                if constexpr (sizeof(T) == 2) {
+                    s[n] = M::mma(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), s[n]);
+                } else {
+                    const float *x = (const float *)&kf, *y = (const float *)&qf[k];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[n] = M::mma(x[e], y[e], s[n]);
-                    }
+                    for (int e = 0; e < 4; ++e) s[n] = M::mma(x[e], y[e], s[n]);
                 }
-            }
-            const bool masked = t0 + KT > all_see;
-            float top = -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = s[n][i] * a.c;
-                    if (masked && t0 + 16 * n + 4 * g + i >= limit) x = -INFINITY;
-                    s[n][i] = x;
-                    top = fmaxf(top, x);
-                }
-            const float m2 = fmaxf(m, row_max16(top));
-            const float mu = m2 == -INFINITY ? 0.f : m2;
-            const float shrink = __builtin_amdgcn_exp2f(m - mu);
-            m = m2;
-            l *= shrink;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - mu);
-                    l += s[n][i];
-                }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[d][i] *= shrink;
-            const char *vt = (const char *)vbuf[b];
-            if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int k = 0; k < NT / 2; ++k) {
-                    const bf16x8 p = pack8(s[2 * k], s[2 * k + 1]);
-                    const int r = 32 * k + 4 * g + (col >> 2);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const int pc = 2 * d + ((col & 3) >> 1), half = 8 * (col & 1);
-                        const bf16x8 v = join_tr(lds_tr(vt + L::vpos(r, pc) * 16 + half),
-                                                 lds_tr(vt + L::vpos(r + 16, pc) * 16 + half));
-                        acc[d] = M::mma(v, p, acc[d]);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const int r = 16 * n + 4 * g + i;
-                            const float v = *(const float *)(vt + L::vpos(r, 4 * d + (col >> 2)) * 16 + 4 * (col & 3));
-                            acc[d] = M::mma(v, s[n][i], acc[d]);
-                        }
             }
         }
-        if (more) store(b ^ 1, t0 + KT);
+        const bool masked = t0 + KT > all_see;
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float x = s[n][i] * a.c;
+                if (masked && t0 + 16 * n + 4 * g + i >= limit) x = -INFINITY;
+                s[n][i] = x;
+                top = fmaxf(top, x);
+            }
+        const float m2 = fmaxf(m, row_max16(top));
+        const float mu = m2 == -INFINITY ? 0.f : m2;
+        const float shrink = __builtin_amdgcn_exp2f(m - mu);
+        m = m2;
+        l *= shrink;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - mu);
+                l += s[n][i];
+            }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[d][i] *= shrink;
+        const char *vt = (const char *)sm.v[b];
+        if constexpr (sizeof(T) == 2) {
+            const char *at = vt + (4 * g + (col >> 2)) * L::PS * 16 + 8 * (col & 3);
+#pragma unroll
+            for (int k = 0; k < NT / 2; ++k) {
+                const bf16x8 p = pack8(s[2 * k], s[2 * k + 1]);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const char *x = at + 32 * k * L::PS * 16 + 32 * d;
+                    acc[d] = M::mma(join_tr(lds_tr(x), lds_tr(x + 16 * L::PS * 16)), p, acc[d]);
+                }
+            }
+        } else {
+            const char *at = vt + 4 * g * L::PS * 16 + 4 * col;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+                        acc[d] = M::mma(*(const float *)(at + (16 * n + i) * L::PS * 16 + 64 * d), s[n][i], acc[d]);
+        }
+    };
+    // the running part joins the sums of those before it
+    auto join = [&]() {
+        float w, wp;
+        join_weights(sum_m, sum_l, m, row_sum16(l), &w, &wp);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            sum[d] = join4(sum[d], acc[d], w, wp);
+            acc[d] = zero4();
+        }
+        m = -INFINITY;
+        l = 0.f;
+    };
+
+    // Two tiles a turn, so that the register sets and buffers are constants; the
+    // loads run past the last tile (as zeros) rather than being skipped, since a
+    // loop that can leave between two register sets makes every wait a wait for all.
+    store(0, t.lo, f0);
+    load(t.lo + 2 * KT, f0);
+    __syncthreads();
+    for (int t0 = t.lo; t0 < t.hi; t0 += 2 * KT) {
+        compute(0, t0);
+        store(1, t0 + KT, f1);
+        load(t0 + 3 * KT, f1);
+        __syncthreads();
+        compute(1, t0 + KT);
+        store(0, t0 + 2 * KT, f0);
+        load(t0 + 4 * KT, f0);
+        if (t0 + 2 * KT < t.hi && (t0 + 2 * KT) % kPromptPart == 0) join();
         __syncthreads();
     }
-    l = row_sum16(l);
-    if (dropped && live) {
-        const int first = max(t.lo, (all_see - t.lo) / KT * KT + t.lo);
+    if (t.hi - t.lo > kPromptPart) {
+        join();
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = sum[d];
+        m = sum_m;
+        l = sum_l;
+    } else {
+        l = row_sum16(l);
+    }
+    if (sm.dropped && live) {
+        const int first = all_see <= t.lo ? t.lo : t.lo + (all_see - t.lo) / KT * KT;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
             add_nonfinite<C, D, PAGED>(a, table_row, seq_row0, t.kvh, first, t.hi, limit, 16 * d + 4 * g, acc[d]);
     }
     if (!live) return;
     if (t.n_parts == 1) {
-        const float inv = l > 0.f || l != l ? a.v_scale / l : 0.f;
+        const float x = row_scale(a, l);
         T *op = (T *)a.o + tok * a.o_stride + (int64_t)head * D;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) store4(op + 16 * d + 4 * g, acc[d] * inv);
+        for (int d = 0; d < DT; ++d) store4(op + 16 * d + 4 * g, acc[d] * x);
     } else if (limit > t.lo) {
         const int64_t slot = (tok * (a.kv_heads * a.group) + head) * a.parts + t.part;
 #pragma unroll
         for (int d = 0; d < DT; ++d) store4(a.part_o + slot * D + 16 * d + 4 * g, acc[d]);
         if (g == 0) a.part_ml[slot] = make_float2(m, l);
     }
+}
+
+template <typename T, typename C, int D, bool PAGED, int NW>
+__global__ __launch_bounds__(64 * NW) void attn_prompt_kernel(AttnArgs a) {
+    __shared__ TileLds<T, D, NW> sm;
+    RowTile t;
+    if (prompt_tile_of<16 * NW>(a, blockIdx.x, &t)) tile_run<T, C, D, PAGED, NW>(a, t, sm);
 }
 
 }  // namespace la
