@@ -11,6 +11,7 @@
 #include "la_host.h"
 #include "attn_tile.h"
 #include "attn_rows.h"
+#include "attn_wide.h"
 #include "blocks.h"
 
 namespace {
@@ -105,62 +106,63 @@ la::KvSource cached(const la_kv_layer *y) {
 
 // --- prompts -----------------------------------------------------------------
 
-// Workgroups that a call of whole rows should have before its keys are left
-// unsplit: one on every CU.
-constexpr int64_t kFullGrid = 256;
-
 struct PromptPlan {
     int64_t tokens = 0, items = 0;      // items: row tiles times parts, of one key head
-    int parts = 1;                      // the most parts of a sequence
+    int64_t slots = 0, joins = 0;       // (row, part) results in the workspace; workgroups that join them
     int32_t max_kv = 0;
-    int waves = 8;                      // of a workgroup: 16 rows each
+    bool wide = false;                  // bf16: attn_wide_kernel; fp32: attn_prompt_kernel of `waves` waves
+    int waves = 8;
 };
 
 la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *kv_len, PromptPlan *p) {
     if (!cu) return fail(LA_ERR_INVALID_ARG, "cu_seqlens_host is required");
     if (cu[0] != 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens[0]=%d", cu[0]);
     const int64_t group = s->q_heads / s->kv_heads;
-    auto keys_of = [&](int i) { return kv_len ? kv_len[i] : cu[i + 1] - cu[i]; };
-    auto tiles = [&](int rows_per_tile, bool split) {
-        int64_t n = 0;
-        for (int i = 0; i < s->n_seqs; ++i)
-            n += up((cu[i + 1] - cu[i]) * group, rows_per_tile) * la::prompt_parts(split, keys_of(i));
-        return n;
-    };
+    int64_t items4 = 0;
     for (int i = 0; i < s->n_seqs; ++i) {
         const int64_t n = (int64_t)cu[i + 1] - cu[i];
         if (n < 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens decreases at sequence %d", i);
         if (n * group > 0x7fffff00) return fail(LA_ERR_INVALID_ARG, "sequence %d is too long for one launch", i);
-        if (keys_of(i) < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys_of(i));
-        p->max_kv = std::max(p->max_kv, keys_of(i));
+        const int32_t keys = kv_len ? kv_len[i] : (int32_t)n;
+        if (keys < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys);
+        p->max_kv = std::max(p->max_kv, keys);
+        const int parts = la::prompt_parts((int)(n * group), keys, s->kv_heads);
+        p->items += up(n * group, la::kPromptRows) * parts;
+        items4 += up(n * group, la::kPromptRows / 2) * parts;
+        if (parts > 1 && n > 0) {
+            p->slots += n * s->q_heads * parts;
+            p->joins += up(n * s->q_heads, 1024 / s->head_dim);
+        }
     }
     p->tokens = cu[s->n_seqs];
-    p->waves = tiles(128, false) * s->kv_heads < kFullGrid ? 4 : 8;
-    p->items = tiles(16 * p->waves, false);
-    if (p->items * s->kv_heads < kFullGrid && p->max_kv > la::kPromptPart) {
-        p->parts = la::prompt_parts(true, p->max_kv);
-        p->items = tiles(16 * p->waves, true);
+    p->wide = s->io_dtype == LA_BF16;
+    // fp32: 64 rows a workgroup while 128 would leave CUs idle
+    if (!p->wide && p->items * s->kv_heads < 256) {
+        p->waves = 4;
+        p->items = items4;
     }
-    if (p->items * s->kv_heads > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "too many row tiles for one launch");
+    if (p->items * s->kv_heads > kMaxGrid || p->slots > kMaxGrid)
+        return fail(LA_ERR_INVALID_ARG, "too many row tiles for one launch");
     return LA_OK;
 }
 
-size_t parts_bytes(int64_t rows, int parts, int d) { return (size_t)rows * parts * (d * sizeof(float) + sizeof(float2)); }
+size_t parts_bytes(int64_t slots, int d) { return (size_t)slots * (d * sizeof(float) + sizeof(float2)); }
 
-void carve_parts(la::AttnArgs *a, void *ws, int64_t rows, int d) {
+void carve_parts(la::AttnArgs *a, void *ws, int64_t slots, int d) {
     a->part_o = (float *)ws;
-    a->part_ml = (float2 *)((char *)ws + (size_t)rows * a->parts * d * sizeof(float));
+    a->part_ml = (float2 *)((char *)ws + (size_t)slots * d * sizeof(float));
 }
 
 template <typename T, typename C, int D, bool PAGED>
 la_status launch_prompt(const la::AttnArgs &a, const PromptPlan &p, hipStream_t st) {
     const dim3 grid((unsigned)(p.items * a.kv_heads));
-    if (p.waves == 4) hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 4>), grid, dim3(256), 0, st, a);
+    if constexpr (sizeof(T) == 2)
+        hipLaunchKernelGGL((la::attn_wide_kernel<C, D, PAGED>), grid, dim3(la::kWideThreads), 0, st, a);
+    else if (p.waves == 4) hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 4>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 8>), grid, dim3(512), 0, st, a);
     if (la_status e = hip_check("attention prompt launch")) return e;
-    if (!a.split) return LA_OK;
-    const int64_t rows = p.tokens * a.kv_heads * a.group;
-    hipLaunchKernelGGL((la::attn_join_prompt_kernel<T, D>), dim3((unsigned)up(rows, 256 / (D / 4))), dim3(256), 0, st, a, rows);
+    if (p.joins == 0) return LA_OK;
+    hipLaunchKernelGGL((la::attn_join_prompt_kernel<T, D>), dim3((unsigned)p.joins), dim3(256), 0, st, a);
     return hip_check("attention join launch");
 }
 
@@ -171,17 +173,15 @@ la_status prompt_of_dim(int d, const la::AttnArgs &a, const PromptPlan &p, hipSt
 
 la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer *layer, const PromptPlan &p, void *ws,
                      size_t ws_bytes, hipStream_t st) {
-    const size_t need = p.parts > 1 ? parts_bytes(p.tokens * s->q_heads, p.parts, s->head_dim) : 0;
+    const size_t need = parts_bytes(p.slots, s->head_dim);
     if (need && (!ws || ws_bytes < need))
         return fail(LA_ERR_WORKSPACE, "workspace of %zu bytes, %zu required", ws ? ws_bytes : 0, need);
     if (need && !aligned16(ws)) return fail(LA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     a.kv_heads = s->kv_heads;
     a.group = s->q_heads / s->kv_heads;
     a.n_seqs = s->n_seqs;
-    a.parts = p.parts;
-    a.split = p.parts > 1;
     a.max_kv = p.max_kv;
-    carve_parts(&a, ws, p.tokens * s->q_heads, s->head_dim);
+    carve_parts(&a, ws, p.slots, s->head_dim);
     (void)hipGetLastError();
     const int d = s->head_dim;
     if (!layer)
@@ -293,7 +293,7 @@ extern "C" {
 size_t la_attn_prefill_workspace_bytes(const la_attn_shape *shape, const int32_t *cu_seqlens_host, const int32_t *kv_len_host) {
     PromptPlan p;
     if (check_attn_shape(shape) || plan_prompt(shape, cu_seqlens_host, kv_len_host, &p)) return 0;
-    return p.parts > 1 ? parts_bytes(p.tokens * shape->q_heads, p.parts, shape->head_dim) : 16;
+    return std::max<size_t>(16, parts_bytes(p.slots, shape->head_dim));
 }
 
 la_status la_attn_prefill(const la_attn_shape *shape, const void *q, const void *k, const void *v, const int32_t *cu_seqlens_dev,
@@ -345,7 +345,7 @@ la_status la_attn_prefill_paged(const la_attn_shape *shape, const la_kv_layer *l
 size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv_len, int64_t max_prefix_len) {
     if (check_decode_sizes(shape, max_kv_len, max_prefix_len)) return 0;
     const DecodePlan p = plan_decode(max_kv_len, max_prefix_len);
-    return p.direct ? 16 : parts_bytes((int64_t)shape->n_seqs * shape->q_heads, p.own_parts + p.prefix_parts, shape->head_dim);
+    return p.direct ? 16 : parts_bytes((int64_t)shape->n_seqs * shape->q_heads * (p.own_parts + p.prefix_parts), shape->head_dim);
 }
 
 la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, const void *q, const int32_t *kv_len_dev,
@@ -370,7 +370,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     a.parts = p.own_parts + p.prefix_parts;
     a.direct = p.direct;
     const int64_t rows = (int64_t)shape->n_seqs * shape->q_heads;
-    const size_t need = p.direct ? 0 : parts_bytes(rows, a.parts, shape->head_dim);
+    const size_t need = p.direct ? 0 : parts_bytes(rows * a.parts, shape->head_dim);
     if (need && (!workspace || ws_bytes < need))
         return fail(LA_ERR_WORKSPACE, "workspace of %zu bytes, %zu required", workspace ? ws_bytes : 0, need);
     if (need && !aligned16(workspace)) return fail(LA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -382,7 +382,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     a.kv_heads = shape->kv_heads;
     a.group = shape->q_heads / shape->kv_heads;
     a.max_kv = (int32_t)max_kv_len;
-    carve_parts(&a, workspace, rows, shape->head_dim);
+    carve_parts(&a, workspace, rows * a.parts, shape->head_dim);
     const int64_t items = rows / a.group * up(a.group, la::kRowsHeads) * p.own_parts;
     int64_t prefix_items = 0;
     if (shared) {

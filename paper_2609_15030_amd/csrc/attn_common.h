@@ -51,24 +51,38 @@ struct AttnArgs {
     float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
     int32_t n_seqs, kv_heads, group, n_groups;
     int32_t max_kv;                // longest kv_len that the tables and the workspace cover
-    int32_t parts;                 // parts the workspace holds for each row
+    int32_t parts;                 // decode: parts the workspace holds for each row
     int32_t prefix_parts;          // decode: of these, the most of a prefix
     int32_t group_tiles;           // decode: row tiles of the largest group
     int32_t prefix_items;          // decode: workgroups of the prefixes, ahead of the others
-    bool split;                    // prompts: a workgroup for every part of the keys
     bool direct;                   // decode: one part each, written straight to o
-    float *part_o;                 // [row][parts][D]
-    float2 *part_ml;               // [row][parts]
+    float *part_o;                 // [slot][D]
+    float2 *part_ml;               // [slot]
 };
 
-// Keys of one part: prompts (also the steps in which an unsplit row joins its
-// sums, so that splitting changes no bit), shared prefixes, a sequence's own.
-constexpr int kPromptPart = 512;
+// Keys of one part of a shared prefix, and of a sequence's own keys (decode).
 constexpr int kPrefixPart = 256;
 constexpr int kOwnPart = 256;
 
-__host__ __device__ inline int prompt_parts(bool split, int keys) {
-    return split && keys > kPromptPart ? (keys + kPromptPart - 1) / kPromptPart : 1;
+// A prompt's keys are cut into parts where its rows alone would leave most of the
+// chip idle: as many as make kPromptGrid workgroups of 128 rows with the
+// sequence's own row tiles, of at least kPromptPart keys.  The rule looks at one
+// sequence only, so its bits do not depend on the batch.
+constexpr int kPromptRows = 128;
+constexpr int kPromptGrid = 128;
+constexpr int kPromptPart = 512;
+
+__host__ __device__ inline int prompt_part_tokens(int rows, int keys, int kv_heads) {
+    const int64_t tiles = (int64_t)((rows + kPromptRows - 1) / kPromptRows) * kv_heads;
+    int parts = tiles > 0 && tiles < kPromptGrid ? (int)(kPromptGrid / tiles) : 1;
+    const int most = (keys + kPromptPart - 1) / kPromptPart;
+    parts = parts < most ? parts : most;
+    return parts <= 1 ? (keys > 64 ? keys : 64) : ((keys + parts - 1) / parts + 63) & ~63;
+}
+
+__host__ __device__ inline int prompt_parts(int rows, int keys, int kv_heads) {
+    const int t = prompt_part_tokens(rows, keys, kv_heads);
+    return keys <= t ? 1 : (keys + t - 1) / t;
 }
 
 // --- 16-byte pieces of rows, as the LDS tiles hold them ---------------------
@@ -210,18 +224,22 @@ __device__ inline void store4(__bf16 *p, f32x4 x) {
 }
 
 // The sequence, and the item within it, of item r when sequence i has
-// items(i) of them: every wave computes it, 64 sequences a step.
-template <typename F>
-__device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
+// items(i) of them; *extra: what the sequences before it have of extra(i).
+// Every wave computes it, 64 sequences a step.
+template <typename F, typename G>
+__device__ inline bool item_of(int n, int r, F items, G extra, int *seq, int *local, int *sum) {
     const int lane = threadIdx.x & 63;
-    int before = 0;
+    int before = 0, before_extra = 0;
     for (int i0 = 0; i0 < n; i0 += 64) {
         const int i = i0 + lane;
-        int x = i < n ? items(i) : 0;
+        int x = i < n ? items(i) : 0, y = i < n ? extra(i) : 0;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
+            const int xu = __shfl_up(x, d), yu = __shfl_up(y, d);
+            if (lane >= d) {
+                x += xu;
+                y += yu;
+            }
         }
         const uint64_t past = __ballot(before + x > r);
         if (past) {
@@ -229,11 +247,19 @@ __device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
             const int start = at ? __shfl(x, at - 1) : 0;
             *seq = __builtin_amdgcn_readfirstlane(i0 + at);
             *local = __builtin_amdgcn_readfirstlane(r - before - start);
+            *sum = __builtin_amdgcn_readfirstlane(before_extra + (at ? __shfl(y, at - 1) : 0));
             return true;
         }
         before += __shfl(x, 63);
+        before_extra += __shfl(y, 63);
     }
     return false;
+}
+
+template <typename F>
+__device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
+    int none;
+    return item_of(n, r, items, [](int) { return 0; }, seq, local, &none);
 }
 
 }  // namespace la

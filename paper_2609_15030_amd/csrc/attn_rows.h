@@ -273,33 +273,25 @@ __global__ __launch_bounds__(kDecodeThreads8, sizeof(T) == 2 ? 4 : 2) void attn_
     }
 }
 
-// Joins the parts of prompt rows, in the order and by the sums in which an
-// unsplit tile joins them.  D / 4 lanes a row.
+// Joins the parts of prompt rows, those of the sequences that have several: D / 4
+// lanes a row, 1,024 / D rows a workgroup.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a, int64_t n_rows) {
-    constexpr int LANES = D / 4, AHEAD = 4;
-    const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+__global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
+    constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 4;
     const int heads = a.kv_heads * a.group;
-    const int64_t tok = min(row, n_rows - 1) / heads;
-    const int head = (int)(row - tok * heads);
-    int lo = 0, n = a.n_seqs;                        // the last sequence that begins at or before the token
-    while (n > 1) {
-        const int half = n >> 1;
-        if (a.cu[lo + half] <= tok) {
-            lo += half;
-            n -= half;
-        } else {
-            n = half;
-        }
-    }
-    if (row >= n_rows) return;
-    const int new_tokens = a.cu[lo + 1] - a.cu[lo], keys = prompt_keys(a, lo);
-    if (prompt_parts(a.split, keys) == 1) return;                // written by its tile
-    const int limit = max(0, keys - new_tokens + (int)(tok - a.cu[lo]) + 1);
-    const int parts = (limit + kPromptPart - 1) / kPromptPart;
-    const float2 *ml = a.part_ml + row * a.parts;
-    const float *po = a.part_o + row * a.parts * D + 4 * lane;
+    auto groups = [&](int i) { return prompt_slots(a, i) ? ((a.cu[i + 1] - a.cu[i]) * heads + ROWS - 1) / ROWS : 0; };
+    int seq, local, slots;
+    if (!item_of(a.n_seqs, (int)blockIdx.x, groups, [&](int i) { return prompt_slots(a, i); }, &seq, &local, &slots)) return;
+    const int lane = threadIdx.x % LANES, row = local * ROWS + threadIdx.x / LANES;
+    const int new_tokens = a.cu[seq + 1] - a.cu[seq], keys = prompt_keys(a, seq);
+    if (row >= new_tokens * heads) return;
+    const int tok = row / heads, head = row - tok * heads;
+    const int pt = prompt_part_tokens(new_tokens * a.group, keys, a.kv_heads);
+    const int stride = prompt_parts(new_tokens * a.group, keys, a.kv_heads);
+    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + pt - 1) / pt;
+    const int64_t slot = slots + (int64_t)row * stride;
+    const float2 *ml = a.part_ml + slot;
+    const float *po = a.part_o + slot * D + 4 * lane;
     float m = -INFINITY, l = 0.f;
     f32x4 x = zero4();
     for (int p0 = 0; p0 < parts; p0 += AHEAD) {
@@ -319,7 +311,7 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a, int64
             x = join4(x, xp[i], w, wp);
         }
     }
-    store4((T *)a.o + tok * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
+    store4((T *)a.o + (a.cu[seq] + tok) * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
 }
 
 // Joins the parts of a single token's row: a workgroup a row, D / 4 lanes a part.

@@ -32,6 +32,8 @@ struct RowTile {
     int keys;                 // keys of the sequence, or of the prefix
     int lo, hi;               // keys of this part
     int part, n_parts;        // n_parts == 1: results go straight to o
+    int64_t slot0;            // else to slot0 + (token * q heads + head) * slot_parts + part
+    int slot_parts;
     bool prefix;
 };
 
@@ -75,9 +77,17 @@ __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     t->pos0 = 0;
     t->keys = group_prefix(a, g, members);
     t->n_parts = 2;
+    t->slot0 = (int64_t)s0 * a.kv_heads * a.group * a.parts;
+    t->slot_parts = a.parts;
     t->lo = t->part * kPrefixPart;
     t->hi = min(t->keys, t->lo + kPrefixPart);
     return t->row0 < t->n_rows && t->lo < t->hi;
+}
+
+// Slots that the parts of sequence i take: none if it has one part.
+__device__ inline int prompt_slots(const AttnArgs &a, int i) {
+    const int rows = (a.cu[i + 1] - a.cu[i]) * a.group, parts = prompt_parts(rows, prompt_keys(a, i), a.kv_heads);
+    return parts > 1 ? rows * a.kv_heads * parts : 0;
 }
 
 template <int ROWS>
@@ -87,25 +97,26 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     t->prefix = false;
     auto items = [&](int i) {
         const int rows = (a.cu[i + 1] - a.cu[i]) * a.group;
-        return (rows + ROWS - 1) / ROWS * prompt_parts(a.split, prompt_keys(a, i));
+        return (rows + ROWS - 1) / ROWS * prompt_parts(rows, prompt_keys(a, i), a.kv_heads);
     };
-    int seq, local;
-    if (!item_of(a.n_seqs, r, items, &seq, &local)) return false;
+    int seq, local, slots;
+    if (!item_of(a.n_seqs, r, items, [&](int i) { return prompt_slots(a, i); }, &seq, &local, &slots)) return false;
     t->seq = seq;
     t->tok0 = a.cu[seq];
     const int rows = (a.cu[seq + 1] - a.cu[seq]) * a.group;
     t->keys = prompt_keys(a, seq);
-    const int tiles = (rows + ROWS - 1) / ROWS;
+    const int tiles = (rows + ROWS - 1) / ROWS, pt = prompt_part_tokens(rows, t->keys, a.kv_heads);
     t->n_rows = rows;
-    t->n_parts = prompt_parts(a.split, t->keys);
+    t->n_parts = t->slot_parts = prompt_parts(rows, t->keys, a.kv_heads);
+    t->slot0 = slots;
     t->part = local / tiles;
     t->row0 = (tiles - 1 - local % tiles) * ROWS;
     t->pos0 = t->keys - rows / a.group;
     t->hi = row_limit(a, *t, min(t->row0 + ROWS, t->n_rows) - 1);
     t->lo = 0;
     if (t->n_parts > 1) {
-        t->lo = t->part * kPromptPart;
-        t->hi = min(t->hi, t->lo + kPromptPart);
+        t->lo = t->part * pt;
+        t->hi = min(t->hi, t->lo + pt);
         return t->lo < t->hi;
     }
     return true;
@@ -161,7 +172,7 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     constexpr int KT = L::KT, NT = KT / 16, DT = D / 16, LOADS = KT / (NW * L::RPL);
     constexpr int NQ = sizeof(T) == 2 ? D / 32 : D / 16;       // 16-byte pieces of a q row for each lane
     constexpr int CB = Piece<T>::N * sizeof(C), RB = D * sizeof(C);    // stored bytes of a piece, of a row
-    static_assert(LOADS >= 1 && LOADS * NW * L::RPL == KT && kPromptPart % (2 * KT) == 0, "key tile");
+    static_assert(LOADS >= 1 && LOADS * NW * L::RPL == KT, "key tile");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -239,10 +250,10 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         }
     };
 
-    f32x4 acc[DT], sum[DT];
+    f32x4 acc[DT];
 #pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] = sum[i] = zero4();
-    float m = -INFINITY, l = 0.f, sum_m = -INFINITY, sum_l = 0.f;
+    for (int i = 0; i < DT; ++i) acc[i] = zero4();
+    float m = -INFINITY, l = 0.f;
     auto compute = [&](int b, int t0) {
         if (t0 >= wave_hi) return;
         f32x4 s[NT];
@@ -311,19 +322,6 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
                         acc[d] = M::mma(*(const float *)(at + (16 * n + i) * L::PS * 16 + 64 * d), s[n][i], acc[d]);
         }
     };
-    // the running part joins the sums of those before it
-    auto join = [&]() {
-        float w, wp;
-        join_weights(sum_m, sum_l, m, row_sum16(l), &w, &wp);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            sum[d] = join4(sum[d], acc[d], w, wp);
-            acc[d] = zero4();
-        }
-        m = -INFINITY;
-        l = 0.f;
-    };
-
     // Two tiles a turn, so that the register sets and buffers are constants; the
     // loads run past the last tile (as zeros) rather than being skipped, since a
     // loop that can leave between two register sets makes every wait a wait for all.
@@ -338,18 +336,9 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         compute(1, t0 + KT);
         store(0, t0 + 2 * KT, f0);
         load(t0 + 4 * KT, f0);
-        if (t0 + 2 * KT < t.hi && (t0 + 2 * KT) % kPromptPart == 0) join();
         __syncthreads();
     }
-    if (t.hi - t.lo > kPromptPart) {
-        join();
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] = sum[d];
-        m = sum_m;
-        l = sum_l;
-    } else {
-        l = row_sum16(l);
-    }
+    l = row_sum16(l);
     if (sm.dropped && live) {
         const int first = all_see <= t.lo ? t.lo : t.lo + (all_see - t.lo) / KT * KT;
 #pragma unroll
@@ -363,7 +352,7 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
 #pragma unroll
         for (int d = 0; d < DT; ++d) store4(op + 16 * d + 4 * g, acc[d] * x);
     } else if (limit > t.lo) {
-        const int64_t slot = (tok * (a.kv_heads * a.group) + head) * a.parts + t.part;
+        const int64_t slot = t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
 #pragma unroll
         for (int d = 0; d < DT; ++d) store4(a.part_o + slot * D + 16 * d + 4 * g, acc[d]);
         if (g == 0) a.part_ml[slot] = make_float2(m, l);
