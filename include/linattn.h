@@ -468,7 +468,7 @@ typedef struct la_attn_shape {
  * int32, may be NULL), reads as zero keys and values and is not written. */
 typedef struct la_kv_layer {
     void *cache;                     /* device [n_blocks, block_bytes], 16-byte aligned */
-    int64_t n_blocks, block_bytes;   /* block_bytes a multiple of 16               */
+    int64_t n_blocks, block_bytes;   /* n_blocks >= 1; block_bytes a multiple of 16 */
     int64_t k_offset, v_offset;      /* multiples of 16                            */
     int32_t block_tokens;            /* a power of two, 16 to 256                  */
     int32_t kv_heads, head_dim;

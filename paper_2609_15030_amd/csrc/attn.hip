@@ -63,7 +63,7 @@ la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
     const int32_t bt = y->block_tokens;
     if (bt < 16 || bt > 256 || (bt & (bt - 1)))
         return fail(LA_ERR_UNSUPPORTED, "block_tokens=%d: powers of two from 16 to 256 are built", bt);
-    if (y->n_blocks < 0 || y->n_blocks > 0x7fffffff) return fail(LA_ERR_INVALID_ARG, "n_blocks=%lld", (long long)y->n_blocks);
+    if (y->n_blocks < 1 || y->n_blocks > 0x7fffffff) return fail(LA_ERR_INVALID_ARG, "n_blocks=%lld", (long long)y->n_blocks);
     const int64_t part = (int64_t)y->kv_heads * bt * y->head_dim * dtype_size(y->dtype);
     if (y->block_bytes < 0 || y->block_bytes % 16 || y->k_offset < 0 || y->v_offset < 0 || y->k_offset % 16 || y->v_offset % 16 ||
         y->k_offset + part > y->block_bytes || y->v_offset + part > y->block_bytes)
@@ -78,7 +78,7 @@ la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
     if (y->max_blocks < 1 || y->max_blocks * bt > 0x7fffff00)
         return fail(LA_ERR_INVALID_ARG, "max_blocks=%lld must be positive and cover fewer than 2^31 tokens", (long long)y->max_blocks);
     if (!y->block_table) return fail(LA_ERR_INVALID_ARG, "block_table is required");
-    if (y->n_blocks > 0 && (!y->cache || !aligned16(y->cache)))
+    if (!y->cache || !aligned16(y->cache))
         return fail(LA_ERR_INVALID_ARG, "cache is required, 16-byte aligned");
     return LA_OK;
 }
@@ -126,7 +126,7 @@ la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *
         const int32_t keys = kv_len ? kv_len[i] : (int32_t)n;
         if (keys < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys);
         p->max_kv = std::max(p->max_kv, keys);
-        const int parts = la::prompt_parts((int)(n * group), keys, s->kv_heads);
+        const int parts = la::prompt_cut((int)(n * group), keys, s->kv_heads).parts;
         p->items += up(n * group, la::kPromptRows) * parts;
         items4 += up(n * group, la::kPromptRows / 2) * parts;
         if (parts > 1 && n > 0) {
@@ -179,6 +179,8 @@ la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer 
     if (need && !aligned16(ws)) return fail(LA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     a.kv_heads = s->kv_heads;
     a.group = s->q_heads / s->kv_heads;
+    a.by_group = la::FastDiv::by((uint32_t)a.group);
+    a.by_kv_heads = la::FastDiv::by((uint32_t)a.kv_heads);
     a.n_seqs = s->n_seqs;
     a.max_kv = p.max_kv;
     carve_parts(&a, ws, p.slots, s->head_dim);
@@ -381,6 +383,8 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     a.n_seqs = shape->n_seqs;
     a.kv_heads = shape->kv_heads;
     a.group = shape->q_heads / shape->kv_heads;
+    a.by_group = la::FastDiv::by((uint32_t)a.group);
+    a.by_kv_heads = la::FastDiv::by((uint32_t)a.kv_heads);
     a.max_kv = (int32_t)max_kv_len;
     carve_parts(&a, workspace, rows * a.parts, shape->head_dim);
     const int64_t items = rows / a.group * up(a.group, la::kRowsHeads) * p.own_parts;

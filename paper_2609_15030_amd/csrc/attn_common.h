@@ -39,6 +39,21 @@ struct KvSource {
     int32_t *err;
 };
 
+// Division of n < 2^31 by a divisor known to the host: a high product, an add and
+// two shifts in place of the 30-odd instructions of a run-time division.
+struct FastDiv {
+    uint32_t m, s1, s2;
+    __host__ static FastDiv by(uint32_t d) {
+        uint32_t l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        return {(uint32_t)((((((uint64_t)1 << l) - d) << 32) / d) + 1), l < 1 ? l : 1u, l < 1 ? 0u : l - 1};
+    }
+    __device__ inline int operator()(int n) const {
+        const uint32_t t = __umulhi(m, (uint32_t)n);
+        return (int)((t + (((uint32_t)n - t) >> s1)) >> s2);
+    }
+};
+
 struct AttnArgs {
     const void *q;
     void *o;
@@ -50,6 +65,7 @@ struct AttnArgs {
     const int32_t *prefix_len;     // decode: shared keys of each group
     float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
     int32_t n_seqs, kv_heads, group, n_groups;
+    FastDiv by_group, by_kv_heads; // row / group, item / kv_heads
     int32_t max_kv;                // longest kv_len that the tables and the workspace cover
     int32_t parts;                 // decode: parts the workspace holds for each row
     int32_t prefix_parts;          // decode: of these, the most of a prefix
@@ -72,17 +88,18 @@ constexpr int kPromptRows = 128;
 constexpr int kPromptGrid = 128;
 constexpr int kPromptPart = 512;
 
-__host__ __device__ inline int prompt_part_tokens(int rows, int keys, int kv_heads) {
-    const int64_t tiles = (int64_t)((rows + kPromptRows - 1) / kPromptRows) * kv_heads;
-    int parts = tiles > 0 && tiles < kPromptGrid ? (int)(kPromptGrid / tiles) : 1;
-    const int most = (keys + kPromptPart - 1) / kPromptPart;
-    parts = parts < most ? parts : most;
-    return parts <= 1 ? (keys > 64 ? keys : 64) : ((keys + parts - 1) / parts + 63) & ~63;
-}
-
-__host__ __device__ inline int prompt_parts(int rows, int keys, int kv_heads) {
-    const int t = prompt_part_tokens(rows, keys, kv_heads);
-    return keys <= t ? 1 : (keys + t - 1) / t;
+// Keys of a part (a multiple of 64) and parts of a sequence of `rows` rows under
+// each key head that reads `keys` keys.
+struct PromptCut {
+    int part, parts;
+};
+__host__ __device__ inline PromptCut prompt_cut(int rows, int keys, int kv_heads) {
+    const uint32_t tiles = (uint32_t)(rows + kPromptRows - 1) / kPromptRows * (uint32_t)kv_heads;
+    const uint32_t most = (uint32_t)(keys + kPromptPart - 1) / kPromptPart;
+    if (tiles == 0 || tiles > kPromptGrid / 2 || most < 2) return {keys, 1};
+    const uint32_t fill = kPromptGrid / tiles, parts = fill < most ? fill : most;
+    const uint32_t part = (((uint32_t)keys + parts - 1) / parts + 63) & ~63u;
+    return {(int)part, (int)(((uint32_t)keys + part - 1) / part)};
 }
 
 // --- 16-byte pieces of rows, as the LDS tiles hold them ---------------------
@@ -223,43 +240,35 @@ __device__ inline void store4(__bf16 *p, f32x4 x) {
     *(bf16x4 *)p = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
 }
 
-// The sequence, and the item within it, of item r when sequence i has
-// items(i) of them; *extra: what the sequences before it have of extra(i).
-// Every wave computes it, 64 sequences a step.
-template <typename F, typename G>
-__device__ inline bool item_of(int n, int r, F items, G extra, int *seq, int *local, int *sum) {
-    const int lane = threadIdx.x & 63;
-    int before = 0, before_extra = 0;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = i0 + lane;
-        int x = i < n ? items(i) : 0, y = i < n ? extra(i) : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int xu = __shfl_up(x, d), yu = __shfl_up(y, d);
-            if (lane >= d) {
-                x += xu;
-                y += yu;
-            }
-        }
-        const uint64_t past = __ballot(before + x > r);
-        if (past) {
-            const int at = __ffsll((unsigned long long)past) - 1;
-            const int start = at ? __shfl(x, at - 1) : 0;
-            *seq = __builtin_amdgcn_readfirstlane(i0 + at);
-            *local = __builtin_amdgcn_readfirstlane(r - before - start);
-            *sum = __builtin_amdgcn_readfirstlane(before_extra + (at ? __shfl(y, at - 1) : 0));
-            return true;
-        }
-        before += __shfl(x, 63);
-        before_extra += __shfl(y, 63);
-    }
-    return false;
+// Inclusive sum over the wave's lanes.
+__device__ inline int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);       // rows of 16: shifts by 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // row ends to the next row, then to the upper half
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
 }
 
+// The sequence of item r when lane's sequence i has items(i): in steps of 64
+// sequences.  Returns the sequence, its lane in the step and the items before it.
 template <typename F>
 __device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
-    int none;
-    return item_of(n, r, items, [](int) { return 0; }, seq, local, &none);
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int x = wave_scan(i0 + lane < n ? items(i0 + lane) : 0);
+        const uint64_t past = __ballot(before + x > r);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            *seq = i0 + at;
+            *local = r - before - (at ? __builtin_amdgcn_readlane(x, at - 1) : 0);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(x, 63);
+    }
+    return false;
 }
 
 }  // namespace la

@@ -278,17 +278,36 @@ __global__ __launch_bounds__(kDecodeThreads8, sizeof(T) == 2 ? 4 : 2) void attn_
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
     constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 4;
-    const int heads = a.kv_heads * a.group;
-    auto groups = [&](int i) { return prompt_slots(a, i) ? ((a.cu[i + 1] - a.cu[i]) * heads + ROWS - 1) / ROWS : 0; };
-    int seq, local, slots;
-    if (!item_of(a.n_seqs, (int)blockIdx.x, groups, [&](int i) { return prompt_slots(a, i); }, &seq, &local, &slots)) return;
+    const int heads = a.kv_heads * a.group, wl = threadIdx.x & 63;
+    int before = 0, slots = 0, seq = -1, local = 0, c0 = 0, new_tokens = 0, keys = 0;
+    PromptCut cut{0, 1};
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        const int i = min(i0 + wl, a.n_seqs - 1);
+        const int b0 = a.cu[i], n = a.cu[i + 1] - b0, k = prompt_keys(a, i);
+        const PromptCut pc = prompt_cut(n * a.group, k, a.kv_heads);
+        const bool in = i0 + wl < a.n_seqs && pc.parts > 1;
+        const int x = wave_scan(in ? (n * heads + ROWS - 1) / ROWS : 0), y = wave_scan(in ? n * heads * pc.parts : 0);
+        const uint64_t past = __ballot(before + x > (int)blockIdx.x);
+        if (!past) {
+            before += __builtin_amdgcn_readlane(x, 63);
+            slots += __builtin_amdgcn_readlane(y, 63);
+            continue;
+        }
+        const int at = __builtin_ctzll(past);
+        seq = i0 + at;
+        local = (int)blockIdx.x - before - (at ? __builtin_amdgcn_readlane(x, at - 1) : 0);
+        slots += at ? __builtin_amdgcn_readlane(y, at - 1) : 0;
+        c0 = __builtin_amdgcn_readlane(b0, at);
+        new_tokens = __builtin_amdgcn_readlane(n, at);
+        keys = __builtin_amdgcn_readlane(k, at);
+        cut = {__builtin_amdgcn_readlane(pc.part, at), __builtin_amdgcn_readlane(pc.parts, at)};
+        break;
+    }
+    if (seq < 0) return;
     const int lane = threadIdx.x % LANES, row = local * ROWS + threadIdx.x / LANES;
-    const int new_tokens = a.cu[seq + 1] - a.cu[seq], keys = prompt_keys(a, seq);
     if (row >= new_tokens * heads) return;
-    const int tok = row / heads, head = row - tok * heads;
-    const int pt = prompt_part_tokens(new_tokens * a.group, keys, a.kv_heads);
-    const int stride = prompt_parts(new_tokens * a.group, keys, a.kv_heads);
-    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + pt - 1) / pt;
+    const int tok = a.by_group(a.by_kv_heads(row)), head = row - tok * heads;
+    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + cut.part - 1) / cut.part, stride = cut.parts;
     const int64_t slot = slots + (int64_t)row * stride;
     const float2 *ml = a.part_ml + slot;
     const float *po = a.part_o + slot * D + 4 * lane;
@@ -311,7 +330,7 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
             x = join4(x, xp[i], w, wp);
         }
     }
-    store4((T *)a.o + (a.cu[seq] + tok) * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
+    store4((T *)a.o + (int64_t)(c0 + tok) * a.o_stride + (int64_t)head * D + 4 * lane, x * row_scale(a, l));
 }
 
 // Joins the parts of a single token's row: a workgroup a row, D / 4 lanes a part.

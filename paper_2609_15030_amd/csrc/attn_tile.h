@@ -29,6 +29,7 @@ struct RowTile {
     int64_t tok0;             // q token of row 0
     int row0, n_rows;         // first row of the tile, rows of the sequence or group
     int pos0;                 // prompts: position of token 0
+    int all_see;              // prompts: keys that the first row sees, and with it every row
     int keys;                 // keys of the sequence, or of the prefix
     int lo, hi;               // keys of this part
     int part, n_parts;        // n_parts == 1: results go straight to o
@@ -40,7 +41,7 @@ struct RowTile {
 // Keys that a row sees.
 __device__ inline int row_limit(const AttnArgs &a, const RowTile &t, int row) {
     if (row >= t.n_rows) return 0;
-    const int tok = row / a.group;
+    const int tok = a.by_group(row);
     if (t.prefix) return max(0, min(t.keys, min(a.kv_len[t.tok0 + tok], a.max_kv)));
     return max(0, min(t.keys, t.pos0 + tok + 1));
 }
@@ -62,8 +63,8 @@ __device__ inline int prompt_keys(const AttnArgs &a, int i) {
 // prompt's longest (last) tiles come first.
 template <int ROWS>
 __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t) {
-    int r = (int)(b / (uint32_t)a.kv_heads);
-    t->kvh = (int)(b - (uint32_t)r * (uint32_t)a.kv_heads);
+    int r = a.by_kv_heads((int)b);
+    t->kvh = (int)b - r * a.kv_heads;
     t->prefix = true;
     const int tile = r % a.group_tiles;
     r /= a.group_tiles;
@@ -84,42 +85,58 @@ __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     return t->row0 < t->n_rows && t->lo < t->hi;
 }
 
-// Slots that the parts of sequence i take: none if it has one part.
-__device__ inline int prompt_slots(const AttnArgs &a, int i) {
-    const int rows = (a.cu[i + 1] - a.cu[i]) * a.group, parts = prompt_parts(rows, prompt_keys(a, i), a.kv_heads);
-    return parts > 1 ? rows * a.kv_heads * parts : 0;
-}
-
+// The work of a prompt call's item.  One load of the lengths serves a step of 64
+// sequences; the item's sequence is then read from its lane.
 template <int ROWS>
 __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t) {
-    const int r = (int)(b / (uint32_t)a.kv_heads);
-    t->kvh = (int)(b - (uint32_t)r * (uint32_t)a.kv_heads);
+    const int lane = threadIdx.x & 63;
+    const int r = a.by_kv_heads((int)b);
+    t->kvh = (int)b - r * a.kv_heads;
     t->prefix = false;
-    auto items = [&](int i) {
-        const int rows = (a.cu[i + 1] - a.cu[i]) * a.group;
-        return (rows + ROWS - 1) / ROWS * prompt_parts(rows, prompt_keys(a, i), a.kv_heads);
-    };
-    int seq, local, slots;
-    if (!item_of(a.n_seqs, r, items, [&](int i) { return prompt_slots(a, i); }, &seq, &local, &slots)) return false;
-    t->seq = seq;
-    t->tok0 = a.cu[seq];
-    const int rows = (a.cu[seq + 1] - a.cu[seq]) * a.group;
-    t->keys = prompt_keys(a, seq);
-    const int tiles = (rows + ROWS - 1) / ROWS, pt = prompt_part_tokens(rows, t->keys, a.kv_heads);
-    t->n_rows = rows;
-    t->n_parts = t->slot_parts = prompt_parts(rows, t->keys, a.kv_heads);
-    t->slot0 = slots;
-    t->part = local / tiles;
-    t->row0 = (tiles - 1 - local % tiles) * ROWS;
-    t->pos0 = t->keys - rows / a.group;
-    t->hi = row_limit(a, *t, min(t->row0 + ROWS, t->n_rows) - 1);
-    t->lo = 0;
-    if (t->n_parts > 1) {
-        t->lo = t->part * pt;
-        t->hi = min(t->hi, t->lo + pt);
-        return t->lo < t->hi;
+    int before = 0, slots = 0;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        const int i = min(i0 + lane, a.n_seqs - 1);
+        const int c0 = a.cu[i], c1 = a.cu[i + 1];
+        const int keys = prompt_keys(a, i), rows = (c1 - c0) * a.group;
+        const PromptCut cut = prompt_cut(rows, keys, a.kv_heads);
+        const bool in = i0 + lane < a.n_seqs;
+        const int x = wave_scan(in ? (rows + ROWS - 1) / ROWS * cut.parts : 0);
+        const int y = wave_scan(in && cut.parts > 1 ? rows * a.kv_heads * cut.parts : 0);
+        const uint64_t past = __ballot(before + x > r);
+        if (!past) {
+            before += __builtin_amdgcn_readlane(x, 63);
+            slots += __builtin_amdgcn_readlane(y, 63);
+            continue;
+        }
+        const int at = __builtin_ctzll(past);
+        const int local = r - before - (at ? __builtin_amdgcn_readlane(x, at - 1) : 0);
+        t->slot0 = slots + (at ? __builtin_amdgcn_readlane(y, at - 1) : 0);
+        t->seq = i0 + at;
+        t->tok0 = __builtin_amdgcn_readlane(c0, at);
+        t->n_rows = __builtin_amdgcn_readlane(rows, at);
+        t->keys = __builtin_amdgcn_readlane(keys, at);
+        t->n_parts = t->slot_parts = __builtin_amdgcn_readlane(cut.parts, at);
+        const int pt = __builtin_amdgcn_readlane(cut.part, at);
+        const int tiles = (t->n_rows + ROWS - 1) / ROWS;
+        t->part = 0;
+        int tile = local;
+        while (tile >= tiles) {                  // few parts: cheaper than a division
+            tile -= tiles;
+            ++t->part;
+        }
+        t->row0 = (tiles - 1 - tile) * ROWS;
+        t->pos0 = t->keys - (__builtin_amdgcn_readlane(c1, at) - (int)t->tok0);
+        t->all_see = row_limit(a, *t, t->row0);
+        t->hi = row_limit(a, *t, min(t->row0 + ROWS, t->n_rows) - 1);
+        t->lo = 0;
+        if (t->n_parts > 1) {
+            t->lo = t->part * pt;
+            t->hi = min(t->hi, t->lo + pt);
+            return t->lo < t->hi;
+        }
+        return true;
     }
-    return true;
+    return false;
 }
 
 // Stored values of v at token `tok`, dims d .. d + 3, of one key head (zero in a
@@ -179,8 +196,9 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     const int row = t.row0 + 16 * wave + col;
     const int limit = row_limit(a, t, row);
     const bool live = row < t.n_rows;
-    const int64_t tok = t.tok0 + (live ? row / a.group : 0);
-    const int head = t.kvh * a.group + (live ? row % a.group : 0);
+    const int row_tok = live ? a.by_group(row) : 0;
+    const int64_t tok = t.tok0 + row_tok;
+    const int head = t.kvh * a.group + (live ? row - row_tok * a.group : 0);
     const int32_t *table_row = PAGED ? a.kv.table + (int64_t)t.seq * a.kv.max_blocks : nullptr;
     const int64_t seq_row0 = PAGED ? 0 : t.tok0;
     const int lrow = lane / L::PPR, lp = lane % L::PPR;

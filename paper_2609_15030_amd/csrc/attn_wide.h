@@ -30,8 +30,21 @@ constexpr float kLag = 8.f;
 // fragment's transposed reads fall on every bank twice).
 template <int D> struct WideLds {
     static constexpr int KT = 64, PPR = D / 8, KS = PPR + 1, VS = PPR + 4;
-    uint4 k[2][KT * KS], v[2][KT * VS];
-    int least[4], dropped;
+    union {
+        struct {
+            uint4 k[2][KT * KS], v[2][KT * VS];
+        };
+        float out[4][32][D + 4];                 // results on their way out; the padding puts 8 rows on different banks
+    };
+    int dropped;
+};
+
+// Where one tile's rows lie in a cache: byte offsets of the four runs of rows that
+// a wave loads, behind the layer's keys (and values), and which of them are in a
+// block that the table does not name.
+template <int LOADS> struct TileRows {
+    int64_t at[LOADS];
+    uint32_t missing;
 };
 
 // Maximum over the two lanes (l, l + 32) of a 32-column accumulator's row.
@@ -54,58 +67,98 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
     const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
 
-    int kid[LOADS], vid[LOADS];                  // block ids of the next tiles to load
-    auto look = [&](int t0, int (&ids)[LOADS]) {
+    // Tile loads.  Packed rows: one resource from the tile's first row to the last
+    // key, rows past it read as zero.  Cached rows: the block ids of a tile are read
+    // from the table a turn before its keys are loaded, and its offsets serve the
+    // keys and, a turn later, the values.  Rows past the last key are whatever the
+    // block (or block 0) holds: a masked tile's weights and values make it nothing.
+    int ids[LOADS];
+    TileRows<LOADS> krows, vrows;
+    auto look = [&](int t0) {
         if constexpr (PAGED) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) ids[i] = block_of(a.kv, table_row, t0 + (4 * i + wave) * RPL, t.hi);
         }
     };
+    auto place = [&](int t0) {
+        if constexpr (PAGED) {
+            const int mask = (1 << a.kv.bt_shift) - 1;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) top = max(top, (uint32_t)ids[i]);
+            krows.missing = 0;
+            if (top >= (uint32_t)a.kv.n_blocks) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i)
+                    if ((uint32_t)ids[i] >= (uint32_t)a.kv.n_blocks) {
+                        if (lane == 0 && a.kv.err) atomicAdd(a.kv.err, 1);
+                        krows.missing |= 1u << i;
+                        ids[i] = 0;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                krows.at[i] = (int64_t)ids[i] * a.kv.block_bytes + (((t.kvh << a.kv.bt_shift) + ((t0 + (4 * i + wave) * RPL) & mask)) * RB);
+        }
+    };
     Raw<C> fk[LOADS], fv[LOADS];
+    auto load = [&](Raw<C> (&f)[LOADS], const char *base, const TileRows<LOADS> &rows, int64_t stride, uint32_t voff, int t0) {
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) f[i] = *(const Raw<C> *)(base + rows.at[i] + voff);
+        } else {
+            const int n = t.hi - t0;
+            const auto res = make_rsrc(base + (n > 0 ? (seq_row0 + t0) * stride : 0) + (int64_t)t.kvh * RB,
+                                       n > 0 ? (uint32_t)(min(n, KT) - 1) * (uint32_t)stride + RB : 0u);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) f[i] = load_piece<C>(res, voff + (uint32_t)((4 * i + wave) * RPL) * (uint32_t)stride);
+        }
+    };
     auto load_k = [&](int t0) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            fk[i] = load_piece<C>(kv_rows<PAGED>(a.kv, PAGED ? kid[i] : 0, seq_row0, t.kvh, RB, t0 + (4 * i + wave) * RPL, RPL, t.hi).k, kvoff);
+        place(t0);
+        load(fk, a.kv.k, krows, a.kv.k_stride, kvoff, t0);
     };
-    auto load_v = [&](int t0) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            fv[i] = load_piece<C>(kv_rows<PAGED>(a.kv, PAGED ? vid[i] : 0, seq_row0, t.kvh, RB, t0 + (4 * i + wave) * RPL, RPL, t.hi).v, vvoff);
+    auto load_v = [&](int t0) { load(fv, a.kv.v, vrows, a.kv.v_stride, vvoff, t0); };
+    // A turn's loads: keys of the tile at t0, values of the tile before it.
+    auto loads = [&](int t0) {
+        vrows = krows;
+        load_v(t0 - KT);
+        load_k(t0);
+        look(t0 + KT);
     };
-    look(t.lo, kid);
+    look(t.lo);
     load_k(t.lo);
-    look(t.lo, vid);
-    load_v(t.lo);
-    look(t.lo + KT, kid);
+    vrows = krows;
+    look(t.lo + KT);
 
     const int row = t.row0 + 32 * wave + col;
     const bool live = row < t.n_rows;
     const int limit = row_limit(a, t, row), edge = min(limit, t.hi);
-    const int64_t tok = t.tok0 + (live ? row / a.group : 0);
-    const int head = t.kvh * a.group + (live ? row % a.group : 0);
+    const int row_tok = live ? a.by_group(row) : 0;
+    const int64_t tok = t.tok0 + row_tok;
+    const int head = t.kvh * a.group + (live ? row - row_tok * a.group : 0);
     bf16x8 qf[KD];
     {
         const __bf16 *qp = (const __bf16 *)a.q + tok * a.q_stride + (int64_t)head * D + 8 * hf;
 #pragma unroll
         for (int k = 0; k < KD; ++k) qf[k] = __builtin_bit_cast(bf16x8, live ? *(const uint4 *)(qp + 16 * k) : make_uint4(0, 0, 0, 0));
     }
-    int least = live ? limit : 0x7fffffff;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d));
-    if (lane == 0) sm.least[wave] = least;
     if (threadIdx.x == 0) sm.dropped = 0;
-    __syncthreads();
-    // the keys that every row of the workgroup sees
-    const int all_see = __builtin_amdgcn_readfirstlane(min(min(sm.least[0], sm.least[1]), min(sm.least[2], sm.least[3])));
+    const int all_see = t.all_see;
 
     auto store_k = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = piece_of<C>(fk[i]);
+        for (int i = 0; i < LOADS; ++i) {
+            uint4 k = piece_of<C>(fk[i]);
+            if (PAGED && krows.missing && (krows.missing >> i & 1)) k = make_uint4(0, 0, 0, 0);
+            sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = k;
+        }
     };
     auto store_v = [&](int b, bool mixed) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             uint4 v = piece_of<C>(fv[i]);
+            if (PAGED && vrows.missing && (vrows.missing >> i & 1)) v = make_uint4(0, 0, 0, 0);
             if (mixed && drop_nonfinite<__bf16>(v)) sm.dropped = 1;
             sm.v[b][((4 * i + wave) * RPL + lrow) * L::VS + lp] = v;
         }
@@ -183,22 +236,17 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     f32x16 s0, s1;
     bf16x8 p0[2], p1[2];
     store_k(0);
-    store_v(0, t.lo + KT > all_see);
-    load_k(t.lo + KT);
-    look(t.lo + KT, vid);
-    look(t.lo + 2 * KT, kid);
+    loads(t.lo + KT);
     __syncthreads();
     scores(0, 0, s0);
     scores(0, 1, s1);
     (void)weights(t.lo, true, s0, p0);           // sums are still zero
     store_k(1);
+    store_v(0, t.lo + KT > all_see);
     __syncthreads();
     int b = 0;
     auto turn = [&](int t0, bool masked) {
-        load_k(t0 + 2 * KT);
-        load_v(t0 + KT);
-        look(t0 + 3 * KT, kid);
-        look(t0 + 2 * KT, vid);
+        loads(t0 + 2 * KT);
         scores(b ^ 1, 0, s0);
         float shrink = weights(t0 + 32, masked, s1, p1);
         product(b, 0, p0);
@@ -216,9 +264,8 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     for (; t0 + 2 * KT <= min(all_see, t.hi); t0 += KT) turn(t0, false);
     for (; t0 < t.hi; t0 += KT) turn(t0, true);
 
-    if (!live) return;
     l += __shfl_xor(l, 32);
-    if (sm.dropped) {
+    if (sm.dropped && live) {
         const int first = all_see <= t.lo ? t.lo : t.lo + (all_see - t.lo) / KT * KT;
 #pragma unroll
         for (int d = 0; d < MT32; ++d)
@@ -230,21 +277,33 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
                 for (int i = 0; i < 4; ++i) acc[d][4 * q + i] = y[i];
             }
     }
+    // Results go out as whole rows, through LDS: a lane holds four dims here and
+    // there of one row, and storing those as they are took as long as two turns.
     const bool whole = t.n_parts == 1;
-    if (!whole && limit <= t.lo) return;
-    const float x = row_scale(a, l);
-    const int64_t slot = t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
-    __bf16 *op = (__bf16 *)a.o + tok * a.o_stride + (int64_t)head * D + 4 * hf;
-    float *pp = a.part_o + slot * D + 4 * hf;
+    const float x = whole ? row_scale(a, l) : 1.f;
+    const int64_t slot = whole ? 0 : t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
+    if (!whole && live && limit > t.lo && hf == 0) a.part_ml[slot] = make_float2(m, l);
 #pragma unroll
     for (int d = 0; d < MT32; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 y = {acc[d][4 * q], acc[d][4 * q + 1], acc[d][4 * q + 2], acc[d][4 * q + 3]};
-            if (whole) store4(op + 32 * d + 8 * q, y * x);
-            else store4(pp + 32 * d + 8 * q, y);
+        for (int q = 0; q < 4; ++q)
+            *(f32x4 *)&sm.out[wave][col][32 * d + 8 * q + 4 * hf] =
+                f32x4{acc[d][4 * q], acc[d][4 * q + 1], acc[d][4 * q + 2], acc[d][4 * q + 3]} * x;
+    // rows of this wave only: its LDS operations are in order
+    constexpr int RL = D / 4, RS = 64 / RL;      // lanes a row, rows a step
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RS) {
+        const int r = r0 + lane / RL, e = lane % RL * 4;
+        const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
+        const int rr = t.row0 + 32 * wave + r;
+        if (rr >= t.n_rows) continue;
+        const int rt = a.by_group(rr), rh = t.kvh * a.group + rr - rt * a.group;
+        if (whole) {
+            store4((__bf16 *)a.o + (t.tok0 + rt) * a.o_stride + (int64_t)rh * D + e, y);
+        } else if (max(0, min(t.keys, t.pos0 + rt + 1)) > t.lo) {
+            store4(a.part_o + (t.slot0 + ((int64_t)rt * (a.kv_heads * a.group) + rh) * t.slot_parts + t.part) * D + e, y);
         }
-    if (!whole && hf == 0) a.part_ml[slot] = make_float2(m, l);
+    }
 }
 
 template <typename C, int D, bool PAGED>

@@ -70,7 +70,7 @@ def test_shapes_are_refused(change, want):
     (dict(kv_heads=4), la.LA_ERR_INVALID_ARG), (dict(head_dim=64), la.LA_ERR_INVALID_ARG),
     (dict(head_dim=80), la.LA_ERR_UNSUPPORTED), (dict(block_tokens=8), la.LA_ERR_UNSUPPORTED),
     (dict(block_tokens=48), la.LA_ERR_UNSUPPORTED), (dict(block_tokens=512), la.LA_ERR_UNSUPPORTED),
-    (dict(n_blocks=-1), la.LA_ERR_INVALID_ARG), (dict(block_bytes=16000), la.LA_ERR_INVALID_ARG),
+    (dict(n_blocks=-1), la.LA_ERR_INVALID_ARG), (dict(n_blocks=0), la.LA_ERR_INVALID_ARG), (dict(block_bytes=16000), la.LA_ERR_INVALID_ARG),
     (dict(v_offset=8), la.LA_ERR_INVALID_ARG), (dict(v_offset=4096), la.LA_ERR_INVALID_ARG),
     (dict(k_offset=-16), la.LA_ERR_INVALID_ARG), (dict(v_offset=65536 - 4096), la.LA_ERR_INVALID_ARG),
     (dict(k_scale=0.0), la.LA_ERR_INVALID_ARG), (dict(k_scale=2.0), la.LA_ERR_INVALID_ARG),
