@@ -23,7 +23,7 @@ template <typename T, int D> struct RowsLds {
         uint4 v[kDecodeWaves][KT * PS];
         float sum[kDecodeWaves][kRowsHeads][D];
     };
-    float2 ml[kDecodeWaves][kRowsHeads];
+    float m[kDecodeWaves][kRowsHeads], l[kDecodeWaves][kRowsHeads];
 };
 
 // Own keys [first, end) of sequence s of a decode call, and the parts of its
@@ -211,37 +211,40 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
             }
         }
         // the waves' results: every wave scales its sums to the common maximum
+        if (g == 0) sm.m[wave][col] = m;
         l = row_sum16(l);
-        if (g == 0) sm.ml[wave][col] = make_float2(m, l);
         __syncthreads();
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, sm.ml[w][col].x);
+        for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, sm.m[w][col]);
         const float scale = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
         if (live) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) *(f32x4 *)&sm.sum[wave][col][16 * d + 4 * g] = acc[d] * scale;
+            if (g == 0) sm.l[wave][col] = l * scale;
         }
         __syncthreads();
+        const int64_t head_row0 = (int64_t)kvh * a.group + h0;
         for (int e = threadIdx.x; e < live_heads * (D / 4); e += kDecodeThreads8) {
             const int h = e / (D / 4), d = e % (D / 4) * 4;
             f32x4 x = zero4();
-            float lt = 0.f, mt = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kDecodeWaves; ++w) mt = fmaxf(mt, sm.ml[w][h].x);
-            const float mh = mt == -INFINITY ? 0.f : mt;
+            float lt = 0.f;
 #pragma unroll
             for (int w = 0; w < kDecodeWaves; ++w) {
                 x += *(const f32x4 *)&sm.sum[w][h][d];
-                lt += sm.ml[w][h].y * __builtin_amdgcn_exp2f(sm.ml[w][h].x - mh);
+                lt += sm.l[w][h];
             }
-            const int64_t head_row = (int64_t)kvh * a.group + h0 + h;
             if (a.direct) {
-                store4((T *)a.o + seq * a.o_stride + head_row * D + d, x * row_scale(a, lt));
+                store4((T *)a.o + seq * a.o_stride + (head_row0 + h) * D + d, x * row_scale(a, lt));
             } else {
-                const int64_t slot = ((int64_t)seq * a.kv_heads * a.group + head_row) * a.parts + pp + part;
+                const int64_t slot = ((int64_t)seq * a.kv_heads * a.group + head_row0 + h) * a.parts + pp + part;
                 store4(a.part_o + slot * D + d, x);
-                if (d == 0) a.part_ml[slot] = make_float2(mt, lt);
+                if (d == 0) {
+                    float mt = sm.m[0][h];
+#pragma unroll
+                    for (int w = 1; w < kDecodeWaves; ++w) mt = fmaxf(mt, sm.m[w][h]);
+                    a.part_ml[slot] = make_float2(mt, lt);
+                }
             }
         }
         // the next item: the next head, part or sequence that has one

@@ -23,6 +23,72 @@ template <typename T, int D> struct AttnTile {
     static constexpr int PIECES = KT * PS;
 };
 
+// A workgroup's loads of key tiles: wave w of NW takes runs of RPL rows, run i at
+// rows (NW i + w) RPL of the tile.
+//
+// Packed rows: one resource from the tile's first row to the last key; rows past
+// it read as zero.  Cached rows: a run lies in one block; the block ids of a tile
+// are read from the table ahead of time (look), and its offsets (place) serve its
+// keys and its values.  Rows past the last key are whatever the block (or block 0)
+// holds there: a masked tile's weights are zero and its values' infinities and
+// NaN dropped.  A block that the table does not name counts, and its rows are
+// made zero on their way to LDS (missing).  Everything but `voff` is uniform.
+template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvLoads {
+    struct Place {
+        int64_t at[LOADS];
+        uint32_t missing;
+    };
+    const int32_t *table_row;
+    int64_t seq_row0;
+    int kvh, hi, wave;
+    int ids[LOADS];
+
+    __device__ inline void look(const KvSource &s, int t0) {
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) ids[i] = block_of(s, table_row, t0 + (NW * i + wave) * RPL, hi);
+        }
+    }
+    __device__ inline void place(const KvSource &s, int t0, Place *p) {
+        if constexpr (PAGED) {
+            const int mask = (1 << s.bt_shift) - 1;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) top = max(top, (uint32_t)ids[i]);
+            p->missing = 0;
+            if (top >= (uint32_t)s.n_blocks) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i)
+                    if ((uint32_t)ids[i] >= (uint32_t)s.n_blocks) {
+                        if ((threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
+                        p->missing |= 1u << i;
+                        ids[i] = 0;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                p->at[i] = (int64_t)ids[i] * s.block_bytes + (((kvh << s.bt_shift) + ((t0 + (NW * i + wave) * RPL) & mask)) * RB);
+        }
+    }
+    __device__ inline void load(Raw<C> (&f)[LOADS], const char *base, const Place &p, int64_t stride, uint32_t voff, int t0, int tile) const {
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) f[i] = *(const Raw<C> *)(base + p.at[i] + voff);
+        } else {
+            const int n = hi - t0;
+            const auto res = make_rsrc(base + (n > 0 ? (seq_row0 + t0) * stride : 0) + (int64_t)kvh * RB,
+                                       n > 0 ? (uint32_t)(min(n, tile) - 1) * (uint32_t)stride + RB : 0u);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) f[i] = load_piece<C>(res, voff + (uint32_t)((NW * i + wave) * RPL) * (uint32_t)stride);
+        }
+    }
+    // Run i's piece as it goes to LDS.
+    __device__ static inline uint4 piece(const Raw<C> &f, const Place &p, int i) {
+        if (PAGED && p.missing && (p.missing >> i & 1)) return make_uint4(0, 0, 0, 0);
+        return piece_of<C>(f);
+    }
+};
+
 // The tile of rows that a workgroup works on (all values uniform).
 struct RowTile {
     int kvh, seq;             // key head; row of the block table
@@ -178,7 +244,12 @@ __device__ inline void add_nonfinite(const AttnArgs &a, const int32_t *table_row
 
 // LDS of a workgroup of NW waves.
 template <typename T, int D, int NW> struct TileLds {
-    uint4 k[2][AttnTile<T, D>::PIECES], v[2][AttnTile<T, D>::PIECES];
+    union {
+        struct {
+            uint4 k[2][AttnTile<T, D>::PIECES], v[2][AttnTile<T, D>::PIECES];
+        };
+        float out[NW][16][D + 4];                // results on their way out; the padding puts 16 rows on different banks
+    };
     int least[NW], dropped;
 };
 
@@ -204,28 +275,19 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     const int lrow = lane / L::PPR, lp = lane % L::PPR;
     const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
     const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
-
-    // Tile x's loads: rows (NW i + wave) RPL + lrow of it.  The block ids of the
-    // tile after it are read from the table meanwhile.
-    int ids[LOADS];
-    auto look = [&](int t0) {
-        if constexpr (PAGED) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) ids[i] = block_of(a.kv, table_row, t0 + (NW * i + wave) * L::RPL, t.hi);
-        }
-    };
-    struct Flight { Raw<C> k[LOADS], v[LOADS]; };
+    using Loads = KvLoads<C, PAGED, NW, L::RPL, LOADS, RB>;
+    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}};
+    struct Flight {
+        Raw<C> k[LOADS], v[LOADS];
+        typename Loads::Place p;
+    } f0, f1;
     auto load = [&](int t0, Flight &f) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const auto res = kv_rows<PAGED>(a.kv, PAGED ? ids[i] : 0, seq_row0, t.kvh, RB, t0 + (NW * i + wave) * L::RPL, L::RPL, t.hi);
-            f.k[i] = load_piece<C>(res.k, kvoff);
-            f.v[i] = load_piece<C>(res.v, vvoff);
-        }
-        look(t0 + KT);
+        ld.place(a.kv, t0, &f.p);
+        ld.load(f.k, a.kv.k, f.p, a.kv.k_stride, kvoff, t0, KT);
+        ld.load(f.v, a.kv.v, f.p, a.kv.v_stride, vvoff, t0, KT);
+        ld.look(a.kv, t0 + KT);
     };
-    look(t.lo);
-    Flight f0, f1;
+    ld.look(a.kv, t.lo);
     load(t.lo, f0);
     load(t.lo + KT, f1);
 
@@ -261,8 +323,8 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = ((NW * i + wave) * L::RPL + lrow) * L::PS + lp;
-            sm.k[b][at] = piece_of<C>(f.k[i]);
-            uint4 v = piece_of<C>(f.v[i]);
+            sm.k[b][at] = Loads::piece(f.k[i], f.p, i);
+            uint4 v = Loads::piece(f.v[i], f.p, i);
             if (mixed && drop_nonfinite<T>(v)) sm.dropped = 1;
             sm.v[b][at] = v;
         }
@@ -363,17 +425,25 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         for (int d = 0; d < DT; ++d)
             add_nonfinite<C, D, PAGED>(a, table_row, seq_row0, t.kvh, first, t.hi, limit, 16 * d + 4 * g, acc[d]);
     }
-    if (!live) return;
-    if (t.n_parts == 1) {
-        const float x = row_scale(a, l);
-        T *op = (T *)a.o + tok * a.o_stride + (int64_t)head * D;
+    // Results go out as whole rows, through LDS (the last barrier is behind every read of its tiles).
+    const bool whole = t.n_parts == 1;
+    const float x = whole ? row_scale(a, l) : 1.f;
+    const int heads = a.kv_heads * a.group;
+    if (!whole && live && limit > t.lo && g == 0)
+        a.part_ml[t.slot0 + ((tok - t.tok0) * heads + head) * t.slot_parts + t.part] = make_float2(m, l);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) store4(op + 16 * d + 4 * g, acc[d] * x);
-    } else if (limit > t.lo) {
-        const int64_t slot = t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
+    for (int d = 0; d < DT; ++d) *(f32x4 *)&sm.out[wave][col][16 * d + 4 * g] = acc[d] * x;
+    constexpr int RL = D / 4, RS = 64 / RL;      // lanes a row, rows a step
 #pragma unroll
-        for (int d = 0; d < DT; ++d) store4(a.part_o + slot * D + 16 * d + 4 * g, acc[d]);
-        if (g == 0) a.part_ml[slot] = make_float2(m, l);
+    for (int r0 = 0; r0 < 16; r0 += RS) {
+        const int r = r0 + lane / RL, e = lane % RL * 4;
+        const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
+        const int rr = t.row0 + 16 * wave + r;
+        if (rr >= t.n_rows) continue;
+        const int rt = a.by_group(rr), rh = t.kvh * a.group + rr - rt * a.group;
+        if (whole) store4((T *)a.o + (t.tok0 + rt) * a.o_stride + (int64_t)rh * D + e, y);
+        else if (row_limit(a, t, rr) > t.lo)
+            store4(a.part_o + (t.slot0 + ((int64_t)rt * heads + rh) * t.slot_parts + t.part) * D + e, y);
     }
 }
 

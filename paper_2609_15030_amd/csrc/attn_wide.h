@@ -39,14 +39,6 @@ template <int D> struct WideLds {
     int dropped;
 };
 
-// Where one tile's rows lie in a cache: byte offsets of the four runs of rows that
-// a wave loads, behind the layer's keys (and values), and which of them are in a
-// block that the table does not name.
-template <int LOADS> struct TileRows {
-    int64_t at[LOADS];
-    uint32_t missing;
-};
-
 // Maximum over the two lanes (l, l + 32) of a 32-column accumulator's row.
 __device__ inline float half_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -67,69 +59,22 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
     const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
 
-    // Tile loads.  Packed rows: one resource from the tile's first row to the last
-    // key, rows past it read as zero.  Cached rows: the block ids of a tile are read
-    // from the table a turn before its keys are loaded, and its offsets serve the
-    // keys and, a turn later, the values.  Rows past the last key are whatever the
-    // block (or block 0) holds: a masked tile's weights and values make it nothing.
-    int ids[LOADS];
-    TileRows<LOADS> krows, vrows;
-    auto look = [&](int t0) {
-        if constexpr (PAGED) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) ids[i] = block_of(a.kv, table_row, t0 + (4 * i + wave) * RPL, t.hi);
-        }
-    };
-    auto place = [&](int t0) {
-        if constexpr (PAGED) {
-            const int mask = (1 << a.kv.bt_shift) - 1;
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) top = max(top, (uint32_t)ids[i]);
-            krows.missing = 0;
-            if (top >= (uint32_t)a.kv.n_blocks) {
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i)
-                    if ((uint32_t)ids[i] >= (uint32_t)a.kv.n_blocks) {
-                        if (lane == 0 && a.kv.err) atomicAdd(a.kv.err, 1);
-                        krows.missing |= 1u << i;
-                        ids[i] = 0;
-                    }
-            }
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                krows.at[i] = (int64_t)ids[i] * a.kv.block_bytes + (((t.kvh << a.kv.bt_shift) + ((t0 + (4 * i + wave) * RPL) & mask)) * RB);
-        }
-    };
+    using Loads = KvLoads<C, PAGED, 4, RPL, LOADS, RB>;
+    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}};
+    typename Loads::Place kplace, vplace;
     Raw<C> fk[LOADS], fv[LOADS];
-    auto load = [&](Raw<C> (&f)[LOADS], const char *base, const TileRows<LOADS> &rows, int64_t stride, uint32_t voff, int t0) {
-        if constexpr (PAGED) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) f[i] = *(const Raw<C> *)(base + rows.at[i] + voff);
-        } else {
-            const int n = t.hi - t0;
-            const auto res = make_rsrc(base + (n > 0 ? (seq_row0 + t0) * stride : 0) + (int64_t)t.kvh * RB,
-                                       n > 0 ? (uint32_t)(min(n, KT) - 1) * (uint32_t)stride + RB : 0u);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) f[i] = load_piece<C>(res, voff + (uint32_t)((4 * i + wave) * RPL) * (uint32_t)stride);
-        }
-    };
-    auto load_k = [&](int t0) {
-        place(t0);
-        load(fk, a.kv.k, krows, a.kv.k_stride, kvoff, t0);
-    };
-    auto load_v = [&](int t0) { load(fv, a.kv.v, vrows, a.kv.v_stride, vvoff, t0); };
     // A turn's loads: keys of the tile at t0, values of the tile before it.
     auto loads = [&](int t0) {
-        vrows = krows;
-        load_v(t0 - KT);
-        load_k(t0);
-        look(t0 + KT);
+        vplace = kplace;
+        ld.load(fv, a.kv.v, vplace, a.kv.v_stride, vvoff, t0 - KT, KT);
+        ld.place(a.kv, t0, &kplace);
+        ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t0, KT);
+        ld.look(a.kv, t0 + KT);
     };
-    look(t.lo);
-    load_k(t.lo);
-    vrows = krows;
-    look(t.lo + KT);
+    ld.look(a.kv, t.lo);
+    ld.place(a.kv, t.lo, &kplace);
+    ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t.lo, KT);
+    ld.look(a.kv, t.lo + KT);
 
     const int row = t.row0 + 32 * wave + col;
     const bool live = row < t.n_rows;
@@ -148,17 +93,12 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
 
     auto store_k = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            uint4 k = piece_of<C>(fk[i]);
-            if (PAGED && krows.missing && (krows.missing >> i & 1)) k = make_uint4(0, 0, 0, 0);
-            sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = k;
-        }
+        for (int i = 0; i < LOADS; ++i) sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = Loads::piece(fk[i], kplace, i);
     };
     auto store_v = [&](int b, bool mixed) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            uint4 v = piece_of<C>(fv[i]);
-            if (PAGED && vrows.missing && (vrows.missing >> i & 1)) v = make_uint4(0, 0, 0, 0);
+            uint4 v = Loads::piece(fv[i], vplace, i);
             if (mixed && drop_nonfinite<__bf16>(v)) sm.dropped = 1;
             sm.v[b][((4 * i + wave) * RPL + lrow) * L::VS + lp] = v;
         }

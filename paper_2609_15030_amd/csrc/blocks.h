@@ -163,19 +163,30 @@ __global__ __launch_bounds__(kBlockThreads) void extend_kernel(BlockPoolArgs p, 
         const int64_t first = e0 + threadIdx.x * E;
         int32_t *at[E];
         int want = 0, total;
+        int i = first < all ? (int)(first / p.max_blocks) : n;
+        int64_t j = first - i * p.max_blocks;
+        int row = i < n ? rows[i] : -1, tokens = i < n ? len[i] : 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             at[e] = nullptr;
-            if (first + e >= all) continue;
-            const int i = (int)((first + e) / p.max_blocks), j = (int)(first + e - i * p.max_blocks);
-            const int row = rows[i], tokens = len[i];
-            const bool bad = row < 0 || row >= p.n_rows || tokens < 0 || tokens > (p.max_blocks << p.bt_shift);
-            if (bad && j == 0) count_error(p);
-            if (row < 0 || row >= p.n_rows || ((int64_t)j << p.bt_shift) >= tokens) continue;
-            int32_t *entry = p.table + row * p.max_blocks + j;
-            if (*entry != -1) continue;
-            at[e] = entry;
-            ++want;
+            if (j == p.max_blocks) {
+                j = 0;
+                ++i;
+                row = i < n ? rows[i] : -1;
+                tokens = i < n ? len[i] : 0;
+            }
+            if (i < n) {
+                const bool none = row < 0 || row >= p.n_rows;
+                if (j == 0 && (none || tokens < 0 || tokens > (p.max_blocks << p.bt_shift))) count_error(p);
+                if (!none && (j << p.bt_shift) < tokens) {
+                    int32_t *entry = p.table + row * p.max_blocks + j;
+                    if (*entry == -1) {
+                        at[e] = entry;
+                        ++want;
+                    }
+                }
+            }
+            ++j;
         }
         int k = taken + block_sum_before(want, &total);
 #pragma unroll

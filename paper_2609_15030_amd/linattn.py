@@ -14,6 +14,7 @@ import os
 from typing import Optional, Sequence
 
 import numpy as np
+import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "liblinattn.so")
@@ -453,38 +454,41 @@ def la_hybrid_restore(kv: LaKvBlocks, boundary_dev, boundary_host, state_pool, s
 # attention over packed or cached keys, and the cache's blocks
 # ---------------------------------------------------------------------------
 
-def _rows_ptr(t, last) -> Optional[int]:
-    """Device pointer of a [tokens, heads, head_dim] tensor whose heads are
-    packed within a token (a slice of a wider projection will do)."""
-    if t is None:
-        return None
+_DTYPES = {torch.bfloat16: LA_BF16, torch.float32: LA_F32, torch.float8_e4m3fn: LA_FP8_E4M3}
+_I32 = torch.int32
+
+
+def _rows_ptr(t, heads: int, dim: int) -> int:
+    """Device pointer of a [tokens, heads, dim] tensor whose heads are packed
+    within a token (a slice of a wider projection will do)."""
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError("expected [tokens, heads, head_dim] with packed heads")
-    if last is not None and t.shape[1:] != last:
-        raise ValueError(f"expected heads of shape {tuple(last)}, got {tuple(t.shape[1:])}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"expected [tokens, {heads}, {dim}], got {tuple(t.shape)}")
+    if not t.is_contiguous() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+        raise ValueError("expected packed heads within a token")
     return t.data_ptr()
 
 
 def _dtype_of(dtype) -> int:
-    import torch
-    try:
-        return {torch.bfloat16: LA_BF16, torch.float32: LA_F32, torch.float8_e4m3fn: LA_FP8_E4M3}[dtype]
-    except KeyError:
-        raise ValueError(f"no library type for {dtype}") from None
+    d = _DTYPES.get(dtype)
+    if d is None:
+        raise ValueError(f"no library type for {dtype}")
+    return d
 
 
 def _token_stride(t) -> int:
-    """Elements from one token to the next (0, packed, where there is one token)."""
-    return t.stride(0) if t.shape[0] > 1 else 0
+    """Elements from one token to the next (0, packed, for packed rows or one token)."""
+    return 0 if t.is_contiguous() or t.shape[0] == 1 else t.stride(0)
 
 
-def _ids(t, what):
-    import torch
-    if t is not None and t.dtype != torch.int32:
-        raise ValueError(f"{what}: expected int32, got {t.dtype}")
-    return t
+def _ids(t, what) -> Optional[int]:
+    """Device pointer of an int32 tensor."""
+    if t is None:
+        return None
+    if t.dtype != _I32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous int32 device tensor")
+    return t.data_ptr()
 
 
 def make_attn_shape(n_seqs, q_heads, kv_heads, head_dim, io_dtype=LA_BF16, scale=None) -> LaAttnShape:
@@ -499,7 +503,6 @@ def make_kv_layer(cache, block_table, block_tokens: int, kv_heads: int, head_dim
     """la_kv_layer over a byte cache [n_blocks, block_bytes] (uint8) and a device
     int32 block table [n_seqs, max_blocks].  dtype: torch.bfloat16, float32 or
     float8_e4m3fn; v_offset None: right behind the keys."""
-    import torch
     if cache.dim() != 2 or cache.dtype != torch.uint8:
         raise ValueError("expected a uint8 cache [n_blocks, block_bytes]")
     if block_table.dim() != 2:
@@ -508,8 +511,8 @@ def make_kv_layer(cache, block_table, block_tokens: int, kv_heads: int, head_dim
     if v_offset is None:
         v_offset = k_offset + kv_heads * block_tokens * head_dim * size
     y = LaKvLayer(_dptr(cache), cache.shape[0], cache.shape[1], k_offset, v_offset, block_tokens, kv_heads, head_dim,
-                  _dtype_of(dtype), k_scale, v_scale, _dptr(_ids(block_table, "block_table")), block_table.shape[1],
-                  _dptr(_ids(err_count, "err_count")))
+                  _dtype_of(dtype), k_scale, v_scale, _ids(block_table, "block_table"), block_table.shape[1],
+                  _ids(err_count, "err_count"))
     y._keep = (cache, block_table, err_count)       # the struct holds raw addresses only
     y._seqs = block_table.shape[0]
     return y
@@ -520,7 +523,7 @@ def make_prefix_groups(cu_group, prefix_len, max_group: int, max_prefix_len: int
     n = prefix_len.numel()
     if cu_group.numel() != n + 1:
         raise ValueError(f"{n} prefix lengths go with {n + 1} group offsets")
-    g = LaPrefixGroups(n, int(max_group), _dptr(_ids(cu_group, "cu_group")), _dptr(_ids(prefix_len, "prefix_len")),
+    g = LaPrefixGroups(n, int(max_group), _ids(cu_group, "cu_group"), _ids(prefix_len, "prefix_len"),
                        int(max_prefix_len))
     g._keep = (cu_group, prefix_len)
     return g
@@ -529,7 +532,6 @@ def make_prefix_groups(cu_group, prefix_len, max_group: int, max_prefix_len: int
 def make_block_pool(cache, block_tokens: int, table, ref_count, free_list, free_count, err_count=None) -> LaBlockPool:
     """la_block_pool over a uint8 cache [n_blocks, block_bytes] and device int32
     table [rows, max_blocks], ref_count, free_list [n_blocks] and free_count [1]."""
-    import torch
     if cache.dim() != 2 or cache.dtype != torch.uint8:
         raise ValueError("expected a uint8 cache [n_blocks, block_bytes]")
     if table.dim() != 2:
@@ -537,31 +539,33 @@ def make_block_pool(cache, block_tokens: int, table, ref_count, free_list, free_
     if ref_count.numel() != cache.shape[0] or free_list.numel() != cache.shape[0] or free_count.numel() != 1:
         raise ValueError("expected ref_count and free_list with one entry a block, free_count with one")
     p = LaBlockPool(_dptr(cache), cache.shape[0], cache.shape[1], table.shape[0], table.shape[1], block_tokens,
-                    _dptr(_ids(table, "table")), _dptr(_ids(ref_count, "ref_count")),
-                    _dptr(_ids(free_list, "free_list")), _dptr(_ids(free_count, "free_count")),
-                    _dptr(_ids(err_count, "err_count")))
+                    _ids(table, "table"), _ids(ref_count, "ref_count"),
+                    _ids(free_list, "free_list"), _ids(free_count, "free_count"),
+                    _ids(err_count, "err_count"))
     p._keep = (cache, table, ref_count, free_list, free_count, err_count)
     return p
 
 
-def _with_strides(shape: LaAttnShape, q, k, v, o) -> LaAttnShape:
-    shape.q_stride, shape.o_stride = _token_stride(q), _token_stride(o)
-    shape.k_stride = 0 if k is None else _token_stride(k)
-    shape.v_stride = 0 if v is None else _token_stride(v)
-    return shape
+def _with_strides(shape: LaAttnShape, q, k, v, o):
+    """The shape with these tensors' token strides: itself, or a copy where they differ."""
+    qs, os_ = _token_stride(q), _token_stride(o)
+    ks, vs = (0, 0) if k is None else (_token_stride(k), _token_stride(v))
+    if shape.q_stride != qs or shape.o_stride != os_ or shape.k_stride != ks or shape.v_stride != vs:
+        shape = LaAttnShape.from_buffer_copy(shape)
+        shape.q_stride, shape.k_stride, shape.v_stride, shape.o_stride = qs, ks, vs, os_
+    return ctypes.byref(shape)
 
 
 def _attn_io(shape: LaAttnShape, q, o, rows):
-    want = (shape.q_heads, shape.head_dim)
     if _dtype_of(q.dtype) != shape.io_dtype or o.dtype != q.dtype:
         raise ValueError("q and o must have the shape's io_dtype")
     if q.shape[0] != rows or o.shape[0] != rows:
         raise ValueError(f"q and o must have {rows} rows")
-    return _rows_ptr(q, want), _rows_ptr(o, want)
+    return _rows_ptr(q, shape.q_heads, shape.head_dim), _rows_ptr(o, shape.q_heads, shape.head_dim)
 
 
 def _ws(workspace):
-    return (0, 0) if workspace is None else (_dptr(workspace), workspace.numel() * workspace.element_size())
+    return (None, 0) if workspace is None else (_dptr(workspace), workspace.numel() * workspace.element_size())
 
 
 def la_attn_prefill_workspace_bytes(shape: LaAttnShape, cu_host: np.ndarray, kv_len_host=None) -> int:
@@ -576,10 +580,10 @@ def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o,
     qp, op = _attn_io(shape, q, o, T)
     if k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != T or v.shape[0] != T:
         raise ValueError(f"k and v must have q's type and {T} rows")
-    kv = (shape.kv_heads, shape.head_dim)
+    H, d = shape.kv_heads, shape.head_dim
     w, n = _ws(workspace)
-    st = _lib.la_attn_prefill(ctypes.byref(_with_strides(shape, q, k, v, o)), qp, _rows_ptr(k, kv), _rows_ptr(v, kv),
-                              _dptr(_ids(cu_dev, "cu_seqlens")), _hptr(cu_host, np.int32), op, w, n, _stream(stream))
+    st = _lib.la_attn_prefill(_with_strides(shape, q, k, v, o), qp, _rows_ptr(k, H, d), _rows_ptr(v, H, d),
+                              _ids(cu_dev, "cu_seqlens"), _hptr(cu_host, np.int32), op, w, n, _stream(stream))
     if check:
         _check(st)
     return st
@@ -591,9 +595,9 @@ def la_attn_prefill_paged(shape: LaAttnShape, layer: LaKvLayer, q, cu_dev, cu_ho
     if layer._seqs < shape.n_seqs:
         raise ValueError("the block table has fewer rows than the call sequences")
     w, n = _ws(workspace)
-    st = _lib.la_attn_prefill_paged(ctypes.byref(_with_strides(shape, q, None, None, o)), ctypes.byref(layer), qp,
-                                    _dptr(_ids(cu_dev, "cu_seqlens")), _hptr(cu_host, np.int32),
-                                    _dptr(_ids(kv_len_dev, "kv_len")), _hptr(kv_len_host, np.int32), op, w, n,
+    st = _lib.la_attn_prefill_paged(_with_strides(shape, q, None, None, o), ctypes.byref(layer), qp,
+                                    _ids(cu_dev, "cu_seqlens"), _hptr(cu_host, np.int32),
+                                    _ids(kv_len_dev, "kv_len"), _hptr(kv_len_host, np.int32), op, w, n,
                                     _stream(stream))
     if check:
         _check(st)
@@ -610,8 +614,8 @@ def la_attn_decode(shape: LaAttnShape, layer: LaKvLayer, q, kv_len_dev, max_kv_l
     if layer._seqs < shape.n_seqs or kv_len_dev.numel() < shape.n_seqs:
         raise ValueError("the block table or kv_len has fewer rows than the call sequences")
     w, n = _ws(workspace)
-    st = _lib.la_attn_decode(ctypes.byref(_with_strides(shape, q, None, None, o)), ctypes.byref(layer), qp,
-                             _dptr(_ids(kv_len_dev, "kv_len")), int(max_kv_len),
+    st = _lib.la_attn_decode(_with_strides(shape, q, None, None, o), ctypes.byref(layer), qp,
+                             _ids(kv_len_dev, "kv_len"), int(max_kv_len),
                              None if groups is None else ctypes.byref(groups), op, w, n, _stream(stream))
     if check:
         _check(st)
@@ -625,10 +629,10 @@ def la_kv_write(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: 
         raise ValueError("k and v must have one type and shape")
     if layer._seqs < n_seqs or kv_len_dev.numel() < n_seqs:
         raise ValueError("the block table or kv_len has fewer rows than the call sequences")
-    kv = (layer.kv_heads, layer.head_dim)
-    st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(k.dtype), _rows_ptr(k, kv), _token_stride(k), _rows_ptr(v, kv),
-                          _token_stride(v), _dptr(_ids(cu_dev, "cu_seqlens")), n_seqs, k.shape[0],
-                          _dptr(_ids(kv_len_dev, "kv_len")), _stream(stream))
+    H, d = layer.kv_heads, layer.head_dim
+    st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(k.dtype), _rows_ptr(k, H, d), _token_stride(k), _rows_ptr(v, H, d),
+                          _token_stride(v), _ids(cu_dev, "cu_seqlens"), n_seqs, k.shape[0],
+                          _ids(kv_len_dev, "kv_len"), _stream(stream))
     if check:
         _check(st)
     return st
@@ -641,7 +645,7 @@ def _same_count(*lists):
 
 
 def la_blocks_copy(pool: LaBlockPool, src_ids, dst_ids, stream=None, check: bool = True) -> int:
-    st = _lib.la_blocks_copy(ctypes.byref(pool), _dptr(_ids(src_ids, "src_ids")), _dptr(_ids(dst_ids, "dst_ids")),
+    st = _lib.la_blocks_copy(ctypes.byref(pool), _ids(src_ids, "src_ids"), _ids(dst_ids, "dst_ids"),
                              _same_count(src_ids, dst_ids), _stream(stream))
     if check:
         _check(st)
@@ -649,8 +653,8 @@ def la_blocks_copy(pool: LaBlockPool, src_ids, dst_ids, stream=None, check: bool
 
 
 def la_blocks_fork(pool: LaBlockPool, parent_rows, child_rows, lens, stream=None, check: bool = True) -> int:
-    st = _lib.la_blocks_fork(ctypes.byref(pool), _dptr(_ids(parent_rows, "parent_rows")),
-                             _dptr(_ids(child_rows, "child_rows")), _dptr(_ids(lens, "lens")),
+    st = _lib.la_blocks_fork(ctypes.byref(pool), _ids(parent_rows, "parent_rows"),
+                             _ids(child_rows, "child_rows"), _ids(lens, "lens"),
                              _same_count(parent_rows, child_rows, lens), _stream(stream))
     if check:
         _check(st)
@@ -658,7 +662,7 @@ def la_blocks_fork(pool: LaBlockPool, parent_rows, child_rows, lens, stream=None
 
 
 def la_blocks_extend(pool: LaBlockPool, rows, lens, stream=None, check: bool = True) -> int:
-    st = _lib.la_blocks_extend(ctypes.byref(pool), _dptr(_ids(rows, "rows")), _dptr(_ids(lens, "lens")),
+    st = _lib.la_blocks_extend(ctypes.byref(pool), _ids(rows, "rows"), _ids(lens, "lens"),
                                _same_count(rows, lens), _stream(stream))
     if check:
         _check(st)
@@ -666,7 +670,7 @@ def la_blocks_extend(pool: LaBlockPool, rows, lens, stream=None, check: bool = T
 
 
 def la_blocks_free(pool: LaBlockPool, rows, stream=None, check: bool = True) -> int:
-    st = _lib.la_blocks_free(ctypes.byref(pool), _dptr(_ids(rows, "rows")), rows.numel(), _stream(stream))
+    st = _lib.la_blocks_free(ctypes.byref(pool), _ids(rows, "rows"), rows.numel(), _stream(stream))
     if check:
         _check(st)
     return st
@@ -680,7 +684,7 @@ def la_blocks_compact(pool: LaBlockPool, workspace, new_ids=None, stream=None, c
     w, n = _ws(workspace)
     if new_ids is not None and new_ids.numel() != pool.n_blocks:
         raise ValueError("expected new_ids with one entry a block")
-    st = _lib.la_blocks_compact(ctypes.byref(pool), _dptr(_ids(new_ids, "new_ids")), w, n, _stream(stream))
+    st = _lib.la_blocks_compact(ctypes.byref(pool), _ids(new_ids, "new_ids"), w, n, _stream(stream))
     if check:
         _check(st)
     return st
