@@ -26,33 +26,42 @@ template <typename T, int D> struct RowsLds {
     float m[kDecodeWaves][kRowsHeads], l[kDecodeWaves][kRowsHeads];
 };
 
-// Own keys [first, end) of sequence s of a decode call, and the parts of its
-// prefix.  Sequences outside every group share nothing.
-__device__ inline void own_keys(const AttnArgs &a, int s, int *first, int *end, int *prefix_parts) {
-    *end = max(0, min(a.kv_len[s], a.max_kv));
-    *first = 0;
-    *prefix_parts = 0;
-    if (!a.cu_group) return;
-    int lo = 0, n = a.n_groups;                     // groups that begin at or before s
-    while (n > 0) {
-        const int half = n >> 1;
-        if (a.cu_group[lo + half] <= s) {
-            lo += half + 1;
-            n -= half + 1;
-        } else {
-            n = half;
+// What a sequence of a decode call has to itself: keys [first, end), and the parts
+// of the prefix before them.
+struct OwnKeys {
+    int first, end, prefix_parts;
+    // Parts of the own keys: they begin at the 16-token line at or before the first.
+    __device__ inline int lo() const { return first & ~15; }
+    __device__ inline int parts() const { return end <= first ? 0 : (end - lo() + kOwnPart - 1) / kOwnPart; }
+};
+
+// Sequence s's own keys, for every lane its s.  Sequences outside every group share
+// nothing.  Up to 64 groups are read at once, one a lane, beside kv_len: a search
+// would be a chain of loads, each as long as memory takes to answer.
+__device__ inline OwnKeys own_keys(const AttnArgs &a, int s) {
+    OwnKeys k{0, 0, 0};
+    const int len = a.kv_len[s];
+    if (!a.cu_group) {
+        k.end = max(0, min(len, a.max_kv));
+        return k;
+    }
+    int shared = 0;
+    for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+        const int n = min(64, a.n_groups - g0), g = g0 + min((int)(threadIdx.x & 63), n - 1);
+        const int c0 = a.cu_group[g], c1 = a.cu_group[g + 1], p = a.prefix_len[g];
+        for (int i = 0; i < n; ++i) {
+            const int b0 = __builtin_amdgcn_readlane(c0, i), b1 = __builtin_amdgcn_readlane(c1, i);
+            if (s >= b0 && s < b1 && b1 - b0 > 1) shared = __builtin_amdgcn_readlane(p, i);
         }
     }
-    if (lo == 0) return;
-    const int s1 = a.cu_group[lo];
-    if (s >= s1) return;
-    *first = min(group_prefix(a, lo - 1, s1 - a.cu_group[lo - 1]), *end);
-    *prefix_parts = (*first + kPrefixPart - 1) / kPrefixPart;
+    k.end = max(0, min(len, a.max_kv));
+    k.first = max(0, min(min(shared, a.prefix_parts * kPrefixPart), k.end));
+    k.prefix_parts = (k.first + kPrefixPart - 1) / kPrefixPart;
+    return k;
 }
-
-// Parts of own keys [first, end): they begin at the 16-token line at or before first.
-__device__ inline int own_parts(int first, int end) {
-    return end <= first ? 0 : (end - (first & ~15) + kOwnPart - 1) / kOwnPart;
+// Lane `at`'s, for all.
+__device__ inline OwnKeys own_keys_of_lane(const OwnKeys &k, int at) {
+    return {__builtin_amdgcn_readlane(k.first, at), __builtin_amdgcn_readlane(k.end, at), __builtin_amdgcn_readlane(k.prefix_parts, at)};
 }
 
 // Workgroup b of n that take the own keys.
@@ -70,37 +79,42 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
     const int col = lane & 15, g = lane >> 4;
     const int tiles = (a.group + kRowsHeads - 1) / kRowsHeads, heads = tiles * a.kv_heads;
     // the call's items (part of a sequence, key head, row tile; the last fastest), and this workgroup's share
-    auto parts_of = [&](int i) {
-        int first, end, pp;
-        own_keys(a, i, &first, &end, &pp);
-        const int n = own_parts(first, end);
-        return a.direct && n == 0 ? 1 : n;
-    };
-    int total = 0;
+    auto parts_of = [&](const OwnKeys &k) { return a.direct ? 1 : k.parts(); };
+    int total = 0, sum = 0;                      // sum: of the last step of 64 sequences, up to each lane
+    OwnKeys lane_keys{0, 0, 0};
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-        int x = i0 + lane < a.n_seqs ? parts_of(i0 + lane) : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-        total += x;
+        lane_keys = own_keys(a, min(i0 + lane, a.n_seqs - 1));
+        sum = wave_scan(i0 + lane < a.n_seqs ? parts_of(lane_keys) : 0);
+        total += __builtin_amdgcn_readlane(sum, 63);
     }
-    total = __builtin_amdgcn_readfirstlane(total) * heads;
-    const int per = total / n_blocks, extra = total - per * n_blocks;
+    const int per = total * heads / n_blocks, extra = total * heads - per * n_blocks;
     int item = b * per + min(b, extra);
     const int stop = item + per + (b < extra);
     if (b == 0 && a.kv.err)
         for (int i = threadIdx.x; i < a.n_seqs; i += kDecodeThreads8)
             if (a.kv_len[i] > a.max_kv) atomicAdd(a.kv.err, 1);
     if (item >= stop) return;
-    int seq, part;
-    if (!item_of(a.n_seqs, item / heads, parts_of, &seq, &part)) return;
-    int at = item % heads;
-    int first, end, pp;
-    own_keys(a, seq, &first, &end, &pp);
+    int seq = 0, part = item / heads, at = item - part * heads, i0 = 0;
+    if (a.n_seqs > 64) {
+        for (; i0 < a.n_seqs; i0 += 64) {        // the step that holds the first item's sequence
+            lane_keys = own_keys(a, min(i0 + lane, a.n_seqs - 1));
+            sum = wave_scan(i0 + lane < a.n_seqs ? parts_of(lane_keys) : 0);
+            const int n = __builtin_amdgcn_readlane(sum, 63);
+            if (part < n) break;
+            part -= n;
+        }
+    }
+    {
+        const int l0 = __builtin_ctzll(__ballot(sum > part));
+        part -= l0 ? __builtin_amdgcn_readlane(sum, l0 - 1) : 0;
+        seq = i0 + l0;
+    }
+    OwnKeys own = own_keys_of_lane(lane_keys, seq - i0);
 
     for (; item < stop; ++item) {
         const int kvh = at / tiles, h0 = (at - kvh * tiles) * kRowsHeads;
-        const int lo = (first & ~15) + part * kOwnPart;
-        const int hi = min(end, lo + kOwnPart);
+        const int lo = own.lo() + part * kOwnPart, first = own.first;
+        const int hi = min(own.end, lo + kOwnPart);
         const int live_heads = min(kRowsHeads, a.group - h0);
         const bool live = col < live_heads;
         const int head = kvh * a.group + h0 + (live ? col : 0);
@@ -237,7 +251,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
             if (a.direct) {
                 store4((T *)a.o + seq * a.o_stride + (head_row0 + h) * D + d, x * row_scale(a, lt));
             } else {
-                const int64_t slot = ((int64_t)seq * a.kv_heads * a.group + head_row0 + h) * a.parts + pp + part;
+                const int64_t slot = ((int64_t)seq * a.kv_heads * a.group + head_row0 + h) * a.parts + own.prefix_parts + part;
                 store4(a.part_o + slot * D + d, x);
                 if (d == 0) {
                     float mt = sm.m[0][h];
@@ -250,12 +264,16 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         // the next item: the next head, part or sequence that has one
         if (++at == heads && item + 1 < stop) {
             at = 0;
-            if (++part >= own_parts(first, end)) {
+            if (++part >= parts_of(own)) {
                 part = 0;
                 do {
-                    ++seq;
-                    own_keys(a, seq, &first, &end, &pp);
-                } while (!a.direct && own_parts(first, end) == 0);
+                    if (++seq >= a.n_seqs) return;
+                    if (seq - i0 == 64) {
+                        i0 += 64;
+                        lane_keys = own_keys(a, min(i0 + lane, a.n_seqs - 1));
+                    }
+                    own = own_keys_of_lane(lane_keys, seq - i0);
+                } while (parts_of(own) == 0);
             }
         }
         __syncthreads();                                        // sums read before the next item's V lands there
@@ -345,9 +363,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     const int set = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const int heads = a.kv_heads * a.group;
     const uint32_t row = blockIdx.x, seq = row / (uint32_t)heads, head = row - seq * (uint32_t)heads;
-    int first, end, pp;
-    own_keys(a, (int)seq, &first, &end, &pp);
-    const int parts = pp + own_parts(first, end);
+    const OwnKeys own = own_keys(a, (int)seq);
+    const int parts = own.prefix_parts + own.parts();
     const float2 *ml = a.part_ml + (int64_t)row * a.parts;
     const float *po = a.part_o + (int64_t)row * a.parts * D + 4 * lane;
     float m = -INFINITY, l = 0.f;
