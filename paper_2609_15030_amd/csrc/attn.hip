@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "linattn.h"
 #include "la_host.h"
@@ -229,7 +230,7 @@ la_status check_decode_sizes(const la_attn_shape *s, int64_t max_kv_len, int64_t
 
 template <typename T, typename C, int D>
 la_status launch_decode(const la::AttnArgs &a, int64_t rows_blocks, hipStream_t st) {
-    hipLaunchKernelGGL((la::attn_decode_kernel<T, C, D>), dim3((unsigned)(a.prefix_items + rows_blocks)), dim3(la::kDecodeThreads8), 0,
+    hipLaunchKernelGGL((la::attn_decode_kernel<T, C, D>), dim3((unsigned)(a.prefix_items + rows_blocks)), dim3(la::kRowsThreads), 0,
                        st, a);
     if (la_status e = hip_check("attention decode launch")) return e;
     if (a.direct) return LA_OK;
@@ -394,7 +395,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
         a.prefix_len = groups->prefix_len_dev;
         a.n_groups = groups->n_groups;
         a.prefix_parts = p.prefix_parts;
-        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, 16 * la::kDecodeWaves);
+        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, shape->io_dtype == LA_F32 ? 16 * la::kDecodeWaves : la::kPromptRows);
         prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups * a.kv_heads;
     }
     if (items > kMaxGrid || rows > kMaxGrid || prefix_items + kRowsGrid > kMaxGrid)

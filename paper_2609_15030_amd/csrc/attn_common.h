@@ -163,29 +163,21 @@ __device__ inline int block_of(const KvSource &s, const int32_t *table_row, int 
     return t < hi ? table_row[t >> s.bt_shift] : 0;
 }
 
-// Keys and values of `rows` tokens from t on, which lie in one block, for one
-// key head, as buffer resources: rows at and past `hi` read as zero, as do those
+// Cached keys and values of `rows` tokens from t on, which lie in block `id`, for
+// one key head, as buffer resources: rows at and past `hi` read as zero, as do those
 // of a block that the table does not name (counted).  All arguments are uniform.
 struct KvRows { __amdgpu_buffer_rsrc_t k, v; };
-template <bool PAGED>
-__device__ inline KvRows kv_rows(const KvSource &s, int id, int64_t seq_row0, int kvh, int row_bytes, int t, int rows, int hi) {
+__device__ inline KvRows kv_rows(const KvSource &s, int id, int kvh, int row_bytes, int t, int rows, int hi) {
     int n = min(hi - t, rows);
-    if constexpr (PAGED) {
-        if ((uint32_t)id >= (uint32_t)s.n_blocks) {
-            if (n > 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
-            id = 0;
-            n = 0;
-        }
-        const int64_t off = (int64_t)id * s.block_bytes +
-                            (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1)));
-        const uint32_t bytes = n > 0 ? (uint32_t)(n * row_bytes) : 0u;
-        return {make_rsrc(s.k + off, bytes), make_rsrc(s.v + off, bytes)};
-    } else {
-        const int64_t row = n > 0 ? seq_row0 + t : 0, head = (int64_t)kvh * row_bytes;
-        const uint32_t kb = n > 0 ? (uint32_t)(n - 1) * (uint32_t)s.k_stride + (uint32_t)row_bytes : 0u;
-        const uint32_t vb = n > 0 ? (uint32_t)(n - 1) * (uint32_t)s.v_stride + (uint32_t)row_bytes : 0u;
-        return {make_rsrc(s.k + row * s.k_stride + head, kb), make_rsrc(s.v + row * s.v_stride + head, vb)};
+    if ((uint32_t)id >= (uint32_t)s.n_blocks) {
+        if (n > 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
+        id = 0;
+        n = 0;
     }
+    const int64_t off = (int64_t)id * s.block_bytes +
+                        (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1)));
+    const uint32_t bytes = n > 0 ? (uint32_t)(n * row_bytes) : 0u;
+    return {make_rsrc(s.k + off, bytes), make_rsrc(s.v + off, bytes)};
 }
 
 // Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a

@@ -1,19 +1,21 @@
 // Attention of single tokens over a cache, and the joining of parts.
 //
 // One launch holds two kinds of workgroups.  The first ones take the shared
-// prefixes, as tiles of rows (attn_tile.h).  The others take the keys that each
-// sequence has to itself, a part at a time, for up to 16 query heads of one key
-// head: every key and value is used once by one wave, so nothing is shared; each
-// of the eight waves takes key tiles of its own, K goes from memory straight into
-// the registers that the product reads, V through LDS of the wave's own (its
-// fragments are columns), and the waves' m, l and sums meet at the end.
+// prefixes, as tiles of rows (attn_wide.h; fp32: attn_tile.h).  The others take
+// the keys that each sequence has to itself, a part at a time, for up to 16 query
+// heads of one key head: every key and value is used once by one wave, so nothing
+// is shared; each of the four waves takes key tiles of its own, K goes from
+// memory straight into the registers that the product reads, V through LDS of the
+// wave's own (its fragments are columns), and the waves' m, l and sums meet at the
+// end.
 #pragma once
 #include "attn_tile.h"
+#include "attn_wide.h"
 
 namespace la {
 
-constexpr int kDecodeWaves = 8;
-constexpr int kDecodeThreads8 = 64 * kDecodeWaves;
+constexpr int kDecodeWaves = 4;
+constexpr int kRowsThreads = 64 * kDecodeWaves;
 constexpr int kRowsHeads = 16;
 
 template <typename T, int D> struct RowsLds {
@@ -91,7 +93,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
     int item = b * per + min(b, extra);
     const int stop = item + per + (b < extra);
     if (b == 0 && a.kv.err)
-        for (int i = threadIdx.x; i < a.n_seqs; i += kDecodeThreads8)
+        for (int i = threadIdx.x; i < a.n_seqs; i += kRowsThreads)
             if (a.kv_len[i] > a.max_kv) atomicAdd(a.kv.err, 1);
     if (item >= stop) return;
     int seq = 0, part = item / heads, at = item - part * heads, i0 = 0;
@@ -136,24 +138,30 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         for (int d = 0; d < DT; ++d) acc[d] = zero4();
         float m = -INFINITY, l = 0.f;
         char *const vt = (char *)sm.v[wave];
-        for (int t0 = lo + wave * KT; t0 < hi; t0 += kDecodeWaves * KT) {
-            uint4 kr[NT][NK], vr[NT][VL];
+        // the wave's tiles: two of them in flight; those past the last key load nothing
+        constexpr int STEP = kDecodeWaves * KT, TILES = kOwnPart / STEP;
+        static_assert(TILES % 2 == 0, "two tiles a turn");
+        struct Flight { uint4 k[NT][NK], v[NT][VL]; } f0, f1;
+        auto load = [&](int t0, Flight &f) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int id = __builtin_amdgcn_readlane(ids, (t0 - lo) / 16 + n);
-                const auto res = kv_rows<true>(a.kv, id, 0, kvh, RB, t0 + 16 * n, 16, hi);
+                const int id = __builtin_amdgcn_readlane(ids, ((t0 - lo) / 16 + n) & (kOwnPart / 16 - 1));
+                const auto res = kv_rows(a.kv, id, kvh, RB, t0 + 16 * n, 16, hi);
 #pragma unroll
-                for (int k = 0; k < NK; ++k) kr[n][k] = buf_load16(res.k, (uint32_t)(col * RB + 16 * g), 64 * k);
+                for (int k = 0; k < NK; ++k) f.k[n][k] = buf_load16(res.k, (uint32_t)(col * RB + 16 * g), 64 * k);
 #pragma unroll
-                for (int i = 0; i < VL; ++i) vr[n][i] = buf_load16(res.v, (uint32_t)(16 * lane), 1024 * i);
+                for (int i = 0; i < VL; ++i) f.v[n][i] = buf_load16(res.v, (uint32_t)(16 * lane), 1024 * i);
             }
+        };
+        auto compute = [&](int t0, const Flight &f) {
+            if (t0 >= hi) return;
             f32x4 s[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 s[n] = zero4();
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
-                    const uint4 x = kr[n][k];
+                    const uint4 x = f.k[n][k];
                     if constexpr (F8) {
                         const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
                         s[n] = M::mma(__builtin_bit_cast(bf16x8, make_uint4(e0.x, e0.y, e1.x, e1.y)),
@@ -174,7 +182,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
 #pragma unroll
                 for (int i = 0; i < VL; ++i) {
                     uint4 *const to = (uint4 *)vt + (16 * n + VR * i + lane / VPR) * PS;
-                    const uint4 x = vr[n][i];
+                    const uint4 x = f.v[n][i];
                     if constexpr (F8) {
                         const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
                         to[2 * (lane % VPR)] = make_uint4(e0.x, e0.y, e1.x, e1.y);
@@ -223,6 +231,16 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
 #pragma unroll
                     for (int d = 0; d < DT; ++d) acc[d] = M::mma(*(const float *)(x + i * PS * 16 + 64 * d), s[0][i], acc[d]);
             }
+        };
+        const int w0 = lo + wave * KT;
+        load(w0, f0);
+        load(w0 + STEP, f1);
+#pragma unroll
+        for (int i = 0; i < TILES; i += 2) {
+            compute(w0 + i * STEP, f0);
+            if (i + 2 < TILES) load(w0 + (i + 2) * STEP, f0);
+            compute(w0 + (i + 1) * STEP, f1);
+            if (i + 3 < TILES) load(w0 + (i + 3) * STEP, f1);
         }
         // the waves' results: every wave scales its sums to the common maximum
         if (g == 0) sm.m[wave][col] = m;
@@ -239,7 +257,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         }
         __syncthreads();
         const int64_t head_row0 = (int64_t)kvh * a.group + h0;
-        for (int e = threadIdx.x; e < live_heads * (D / 4); e += kDecodeThreads8) {
+        for (int e = threadIdx.x; e < live_heads * (D / 4); e += kRowsThreads) {
             const int h = e / (D / 4), d = e % (D / 4) * 4;
             f32x4 x = zero4();
             float lt = 0.f;
@@ -281,14 +299,18 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
 }
 
 template <typename T, typename C, int D>
-__global__ __launch_bounds__(kDecodeThreads8, sizeof(T) == 2 ? 4 : 2) void attn_decode_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kRowsThreads, 2) void attn_decode_kernel(AttnArgs a) {
+    constexpr bool WIDE = sizeof(T) == 2;
+    constexpr int ROWS = WIDE ? kPromptRows : 16 * kDecodeWaves;
     __shared__ union Lds {
-        TileLds<T, D, kDecodeWaves> tile;
+        std::conditional_t<WIDE, WideLds<D>, TileLds<T, D, kDecodeWaves>> tile;
         RowsLds<T, D> rows;
     } sm;
     if ((int)blockIdx.x < a.prefix_items) {
         RowTile t;
-        if (prefix_tile_of<16 * kDecodeWaves>(a, blockIdx.x, &t)) tile_run<T, C, D, true, kDecodeWaves>(a, t, sm.tile);
+        if (!prefix_tile_of<ROWS>(a, blockIdx.x, &t)) return;
+        if constexpr (WIDE) wide_run<C, D, true>(a, t, sm.tile);
+        else tile_run<T, C, D, true, kDecodeWaves>(a, t, sm.tile);
     } else {
         rows_run<T, C, D>(a, (int)blockIdx.x - a.prefix_items, (int)gridDim.x - a.prefix_items, sm.rows);
     }

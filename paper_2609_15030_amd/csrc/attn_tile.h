@@ -95,7 +95,7 @@ struct RowTile {
     int64_t tok0;             // q token of row 0
     int row0, n_rows;         // first row of the tile, rows of the sequence or group
     int pos0;                 // prompts: position of token 0
-    int all_see;              // prompts: keys that the first row sees, and with it every row
+    int all_see;              // keys that every row of the tile sees
     int keys;                 // keys of the sequence, or of the prefix
     int lo, hi;               // keys of this part
     int part, n_parts;        // n_parts == 1: results go straight to o
@@ -115,7 +115,7 @@ __device__ inline int row_limit(const AttnArgs &a, const RowTile &t, int row) {
 // Shared keys of a group: none if it has only one member (its keys are then all its own).
 __device__ inline int group_prefix(const AttnArgs &a, int g, int members) {
     if (members < 2) return 0;
-    return max(0, min(a.prefix_len[g], a.prefix_parts * kPrefixPart));
+    return max(0, min(a.prefix_len[g], min(a.prefix_parts * kPrefixPart, a.max_kv)));
 }
 
 // Keys of sequence i of a prompt call.
@@ -148,7 +148,14 @@ __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     t->slot_parts = a.parts;
     t->lo = t->part * kPrefixPart;
     t->hi = min(t->keys, t->lo + kPrefixPart);
-    return t->row0 < t->n_rows && t->lo < t->hi;
+    if (t->row0 >= t->n_rows || t->lo >= t->hi) return false;
+    const int first = a.by_group(t->row0), last = a.by_group(min(t->row0 + ROWS, t->n_rows) - 1);
+    int least = t->keys;
+    for (int s = first + (int)(threadIdx.x & 63); s <= last; s += 64) least = min(least, a.kv_len[s0 + s]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
+    t->all_see = max(0, __builtin_amdgcn_readfirstlane(least));
+    return true;
 }
 
 // The work of a prompt call's item.  One load of the lengths serves a step of 64
@@ -250,7 +257,7 @@ template <typename T, int D, int NW> struct TileLds {
         };
         float out[NW][16][D + 4];                // results on their way out; the padding puts 16 rows on different banks
     };
-    int least[NW], dropped;
+    int dropped;
 };
 
 template <typename T, typename C, int D, bool PAGED, int NW>
@@ -300,23 +307,13 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
             qf[s] = live ? *(const uint4 *)(qp + p * Piece<T>::N) : make_uint4(0, 0, 0, 0);
         }
     }
-    // the keys that every row of the workgroup sees, and the most that a row of the wave sees
-    {
-        int lo = live ? limit : 0x7fffffff;
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) lo = min(lo, __shfl_xor(lo, d));
-        if (lane == 0) sm.least[wave] = lo;
-        if (threadIdx.x == 0) sm.dropped = 0;
-    }
-    int wave_hi = limit;
+    const int all_see = t.all_see;
+    int wave_hi = limit;                         // the most keys that a row of the wave sees
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) wave_hi = max(wave_hi, __shfl_xor(wave_hi, d));
     wave_hi = __builtin_amdgcn_readfirstlane(min(wave_hi, t.hi));
+    if (threadIdx.x == 0) sm.dropped = 0;
     __syncthreads();
-    int all_see = sm.least[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) all_see = min(all_see, sm.least[w]);
-    all_see = __builtin_amdgcn_readfirstlane(all_see);
 
     auto store = [&](int b, int t0, const Flight &f) {
         const bool mixed = t0 + KT > all_see;

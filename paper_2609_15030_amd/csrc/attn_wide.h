@@ -1,5 +1,5 @@
-// Causal attention of bf16 prompts: workgroups of 128 rows, four waves of 32, over
-// 64-key tiles in LDS; two workgroups share a CU.
+// Attention of 128-row tiles in bf16, four waves of 32 rows, over 64-key tiles in
+// LDS; two workgroups share a CU.  Prompts, and the shared prefix of decode groups.
 //
 // 32x32x16 products: a K or V fragment that a wave reads from LDS serves 32 rows
 // (16 a wave, as in attn_tile.h, is bound by LDS: 579 against 956 TFLOP/s for
@@ -235,12 +235,12 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     for (int r0 = 0; r0 < 32; r0 += RS) {
         const int r = r0 + lane / RL, e = lane % RL * 4;
         const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
-        const int rr = t.row0 + 32 * wave + r;
+        const int rr = t.row0 + 32 * wave + r, seen = __shfl(limit, r);
         if (rr >= t.n_rows) continue;
         const int rt = a.by_group(rr), rh = t.kvh * a.group + rr - rt * a.group;
         if (whole) {
             store4((__bf16 *)a.o + (t.tok0 + rt) * a.o_stride + (int64_t)rh * D + e, y);
-        } else if (max(0, min(t.keys, t.pos0 + rt + 1)) > t.lo) {
+        } else if (seen > t.lo) {
             store4(a.part_o + (t.slot0 + ((int64_t)rt * (a.kv_heads * a.group) + rh) * t.slot_parts + t.part) * D + e, y);
         }
     }
