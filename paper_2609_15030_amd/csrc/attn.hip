@@ -127,7 +127,7 @@ la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *
         const int32_t keys = kv_len ? kv_len[i] : (int32_t)n;
         if (keys < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys);
         p->max_kv = std::max(p->max_kv, keys);
-        const int parts = la::prompt_cut((int)(n * group), keys, s->kv_heads).parts;
+        const int parts = la::prompt_cut((int)(n * group), keys, s->kv_heads, la::prompt_grid(s->io_dtype == LA_F32)).parts;
         p->items += up(n * group, la::kPromptRows) * parts;
         items4 += up(n * group, la::kPromptRows / 2) * parts;
         if (parts > 1 && n > 0) {
@@ -184,6 +184,7 @@ la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer 
     a.by_kv_heads = la::FastDiv::by((uint32_t)a.kv_heads);
     a.n_seqs = s->n_seqs;
     a.max_kv = p.max_kv;
+    a.prompt_grid = la::prompt_grid(s->io_dtype == LA_F32);
     carve_parts(&a, ws, p.slots, s->head_dim);
     (void)hipGetLastError();
     const int d = s->head_dim;

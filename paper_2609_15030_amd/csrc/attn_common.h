@@ -66,6 +66,7 @@ struct AttnArgs {
     float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
     int32_t n_seqs, kv_heads, group, n_groups;
     FastDiv by_group, by_kv_heads; // row / group, item / kv_heads
+    uint32_t prompt_grid;          // prompts: see prompt_cut
     int32_t max_kv;                // longest kv_len that the tables and the workspace cover
     int32_t parts;                 // decode: parts the workspace holds for each row
     int32_t prefix_parts;          // decode: of these, the most of a prefix
@@ -80,24 +81,24 @@ struct AttnArgs {
 constexpr int kPrefixPart = 256;
 constexpr int kOwnPart = 256;
 
-// A prompt's keys are cut into parts where its rows alone would leave most of the
-// chip idle: as many as make kPromptGrid workgroups of 128 rows with the
+// A prompt's keys are cut into parts where its rows alone would leave much of the
+// chip idle: as many as make prompt_grid workgroups of 128 rows with the
 // sequence's own row tiles, of at least kPromptPart keys.  The rule looks at one
 // sequence only, so its bits do not depend on the batch.
 constexpr int kPromptRows = 128;
-constexpr int kPromptGrid = 128;
-constexpr int kPromptPart = 512;
+constexpr int kPromptPart = 256;
+__host__ __device__ inline uint32_t prompt_grid(bool f32) { return f32 ? 1024 : 256; }
 
 // Keys of a part (a multiple of 64) and parts of a sequence of `rows` rows under
 // each key head that reads `keys` keys.
 struct PromptCut {
     int part, parts;
 };
-__host__ __device__ inline PromptCut prompt_cut(int rows, int keys, int kv_heads) {
+__host__ __device__ inline PromptCut prompt_cut(int rows, int keys, int kv_heads, uint32_t grid) {
     const uint32_t tiles = (uint32_t)(rows + kPromptRows - 1) / kPromptRows * (uint32_t)kv_heads;
     const uint32_t most = (uint32_t)(keys + kPromptPart - 1) / kPromptPart;
-    if (tiles == 0 || tiles > kPromptGrid / 2 || most < 2) return {keys, 1};
-    const uint32_t fill = kPromptGrid / tiles, parts = fill < most ? fill : most;
+    if (tiles == 0 || tiles > grid / 2 || most < 2) return {keys, 1};
+    const uint32_t fill = grid / tiles, parts = fill < most ? fill : most;
     const uint32_t part = (((uint32_t)keys + parts - 1) / parts + 63) & ~63u;
     return {(int)part, (int)(((uint32_t)keys + part - 1) / part)};
 }
@@ -157,28 +158,36 @@ template <typename T> __device__ inline bool drop_nonfinite(uint4 &x) {
     return any;
 }
 
-// A block id read from the table for token t (0 past the last key): prefetched
-// ahead of the loads that use it.
-__device__ inline int block_of(const KvSource &s, const int32_t *table_row, int t, int hi) {
-    return t < hi ? table_row[t >> s.bt_shift] : 0;
-}
-
-// Cached keys and values of `rows` tokens from t on, which lie in block `id`, for
-// one key head, as buffer resources: rows at and past `hi` read as zero, as do those
-// of a block that the table does not name (counted).  All arguments are uniform.
-struct KvRows { __amdgpu_buffer_rsrc_t k, v; };
-__device__ inline KvRows kv_rows(const KvSource &s, int id, int kvh, int row_bytes, int t, int rows, int hi) {
-    int n = min(hi - t, rows);
-    if ((uint32_t)id >= (uint32_t)s.n_blocks) {
-        if (n > 0 && (threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
-        id = 0;
-        n = 0;
+// Byte offsets of runs of 16 cached tokens behind a layer's keys (and values), for
+// one key head: lane j holds run j of the 1,024 tokens from `base` on.  A run lies
+// in one block; its offset is read from its lane when it is needed, which takes two
+// instructions where a table entry read then and there took a scalar load (whose
+// wait is also one for every LDS read in flight) and some twenty instructions.  Runs
+// past the last key are at block 0's offset; those in a block that the table does not
+// name too, and are in `bad`.
+constexpr int kRunTokens = 16;
+struct Runs {
+    int64_t at;
+    uint64_t bad;
+    __device__ static inline int fetch(const KvSource &s, const int32_t *table_row, int base, int hi) {
+        const int t = base + kRunTokens * (int)(threadIdx.x & 63);
+        return t < hi ? table_row[t >> s.bt_shift] : 0;
     }
-    const int64_t off = (int64_t)id * s.block_bytes +
-                        (int64_t)row_bytes * (((int64_t)kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1)));
-    const uint32_t bytes = n > 0 ? (uint32_t)(n * row_bytes) : 0u;
-    return {make_rsrc(s.k + off, bytes), make_rsrc(s.v + off, bytes)};
-}
+    __device__ inline void set(const KvSource &s, int id, int base, int kvh, int row_bytes) {
+        const bool ok = (uint32_t)id < (uint32_t)s.n_blocks;
+        bad = __ballot(!ok);
+        if (!ok && s.err) atomicAdd(s.err, 1);
+        const int t = base + kRunTokens * (int)(threadIdx.x & 63);
+        at = (int64_t)(ok ? id : 0) * s.block_bytes +
+             (int64_t)(((kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1))) * row_bytes);
+    }
+    __device__ inline int64_t run(int r) const {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), r);
+        return (int64_t)((uint64_t)hi << 32 | lo);
+    }
+    __device__ inline bool named(int r) const { return !(bad >> r & 1); }
+};
 
 // Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a
 // q row of a 16-column accumulator.

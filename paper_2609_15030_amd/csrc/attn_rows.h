@@ -120,9 +120,10 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         const int live_heads = min(kRowsHeads, a.group - h0);
         const bool live = col < live_heads;
         const int head = kvh * a.group + h0 + (live ? col : 0);
-        // block ids of the part's runs of 16 keys, one a lane
-        static_assert(kOwnPart / 16 <= 64, "a lane for each run of 16 keys");
-        const int ids = block_of(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo + 16 * (lane & (kOwnPart / 16 - 1)), hi);
+        // the part's runs of 16 keys, one a lane
+        static_assert(kOwnPart <= 64 * kRunTokens, "a lane for each run");
+        Runs runs;
+        runs.set(a.kv, Runs::fetch(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo, hi), lo, kvh, RB);
         uint4 qf[NQ];
         {
             const T *qp = (const T *)a.q + seq * a.q_stride + (int64_t)head * D;
@@ -145,12 +146,14 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         auto load = [&](int t0, Flight &f) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int id = __builtin_amdgcn_readlane(ids, ((t0 - lo) / 16 + n) & (kOwnPart / 16 - 1));
-                const auto res = kv_rows(a.kv, id, kvh, RB, t0 + 16 * n, 16, hi);
+                const int r = ((t0 - lo) / kRunTokens + n) & 63, rows = min(hi - t0 - 16 * n, 16);
+                const int64_t at = runs.run(r);
+                const uint32_t bytes = rows > 0 && runs.named(r) ? (uint32_t)(rows * RB) : 0u;    // the others read as zero
+                const auto kres = make_rsrc(a.kv.k + at, bytes), vres = make_rsrc(a.kv.v + at, bytes);
 #pragma unroll
-                for (int k = 0; k < NK; ++k) f.k[n][k] = buf_load16(res.k, (uint32_t)(col * RB + 16 * g), 64 * k);
+                for (int k = 0; k < NK; ++k) f.k[n][k] = buf_load16(kres, (uint32_t)(col * RB + 16 * g), 64 * k);
 #pragma unroll
-                for (int i = 0; i < VL; ++i) f.v[n][i] = buf_load16(res.v, (uint32_t)(16 * lane), 1024 * i);
+                for (int i = 0; i < VL; ++i) f.v[n][i] = buf_load16(vres, (uint32_t)(16 * lane), 1024 * i);
             }
         };
         auto compute = [&](int t0, const Flight &f) {
@@ -327,7 +330,7 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
         const int i = min(i0 + wl, a.n_seqs - 1);
         const int b0 = a.cu[i], n = a.cu[i + 1] - b0, k = prompt_keys(a, i);
-        const PromptCut pc = prompt_cut(n * a.group, k, a.kv_heads);
+        const PromptCut pc = prompt_cut(n * a.group, k, a.kv_heads, a.prompt_grid);
         const bool in = i0 + wl < a.n_seqs && pc.parts > 1;
         const int x = wave_scan(in ? (n * heads + ROWS - 1) / ROWS : 0), y = wave_scan(in ? n * heads * pc.parts : 0);
         const uint64_t past = __ballot(before + x > (int)blockIdx.x);

@@ -23,17 +23,18 @@ template <typename T, int D> struct AttnTile {
     static constexpr int PIECES = KT * PS;
 };
 
-// A workgroup's loads of key tiles: wave w of NW takes runs of RPL rows, run i at
-// rows (NW i + w) RPL of the tile.
+// A workgroup's loads of key tiles (of 64 keys, or 32): wave w of NW takes runs of
+// RPL rows, run i at rows (NW i + w) RPL of the tile.
 //
 // Packed rows: one resource from the tile's first row to the last key; rows past
-// it read as zero.  Cached rows: a run lies in one block; the block ids of a tile
-// are read from the table ahead of time (look), and its offsets (place) serve its
-// keys and its values.  Rows past the last key are whatever the block (or block 0)
-// holds there: a masked tile's weights are zero and its values' infinities and
-// NaN dropped.  A block that the table does not name counts, and its rows are
-// made zero on their way to LDS (missing).  Everything but `voff` is uniform.
+// it read as zero.  Cached rows: at the tile's offsets (place), which serve its
+// keys and its values.  Rows past the last key are whatever the block holds there:
+// a masked tile's weights are zero and its values' infinities and NaN dropped.  Rows
+// of a block that the table does not name are made zero on their way to LDS
+// (missing).  Everything but `voff` is uniform.
 template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvLoads {
+    static constexpr int STEP = NW * RPL;        // rows from one run of a wave to the next
+    static_assert(STEP % kRunTokens == 0 || kRunTokens % STEP == 0, "a wave's rows lie in one run of 16");
     struct Place {
         int64_t at[LOADS];
         uint32_t missing;
@@ -41,42 +42,46 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
     const int32_t *table_row;
     int64_t seq_row0;
     int kvh, hi, wave;
-    int ids[LOADS];
+    Runs runs;
+    int base, next;                              // first token of `runs`; the lane's block id of the 1,024 tokens behind
 
-    __device__ inline void look(const KvSource &s, int t0) {
+    __device__ inline void begin(const KvSource &s, int lo) {
         if constexpr (PAGED) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) ids[i] = block_of(s, table_row, t0 + (NW * i + wave) * RPL, hi);
+            base = lo & ~(64 * kRunTokens - 1);
+            const int id = Runs::fetch(s, table_row, base, hi);
+            next = Runs::fetch(s, table_row, base + 64 * kRunTokens, hi);
+            runs.set(s, id, base, kvh, RB);
         }
     }
+    // The place of tile t0; tiles come in order.
     __device__ inline void place(const KvSource &s, int t0, Place *p) {
         if constexpr (PAGED) {
-            const int mask = (1 << s.bt_shift) - 1;
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) top = max(top, (uint32_t)ids[i]);
+            if (t0 - base >= 64 * kRunTokens) {
+                base += 64 * kRunTokens;
+                runs.set(s, next, base, kvh, RB);
+                next = Runs::fetch(s, table_row, base + 64 * kRunTokens, hi);
+            }
+            const int r0 = ((t0 - base) + wave * RPL) / kRunTokens;
             p->missing = 0;
-            if (top >= (uint32_t)s.n_blocks) {
+            if (runs.bad) {
 #pragma unroll
-                for (int i = 0; i < LOADS; ++i)
-                    if ((uint32_t)ids[i] >= (uint32_t)s.n_blocks) {
-                        if ((threadIdx.x & 63) == 0 && s.err) atomicAdd(s.err, 1);
-                        p->missing |= 1u << i;
-                        ids[i] = 0;
-                    }
+                for (int i = 0; i < LOADS; ++i) p->missing |= (uint32_t)!runs.named(r0 + i * STEP / kRunTokens) << i;
             }
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                p->at[i] = (int64_t)ids[i] * s.block_bytes + (((kvh << s.bt_shift) + ((t0 + (NW * i + wave) * RPL) & mask)) * RB);
+            for (int i = 0; i < LOADS; ++i) p->at[i] = runs.run(r0 + i * STEP / kRunTokens) + i * STEP % kRunTokens * RB;
         }
     }
-    __device__ inline void load(Raw<C> (&f)[LOADS], const char *base, const Place &p, int64_t stride, uint32_t voff, int t0, int tile) const {
+    // A lane's byte offset within its run, from its row of the RPL and piece.
+    __device__ inline uint32_t voff(int row, int64_t stride, int piece_at) const {
+        return (uint32_t)(PAGED ? (wave * RPL % kRunTokens + row) * RB : row * (int)stride) + (uint32_t)piece_at;
+    }
+    __device__ inline void load(Raw<C> (&f)[LOADS], const char *from, const Place &p, int64_t stride, uint32_t voff, int t0, int tile) const {
         if constexpr (PAGED) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) f[i] = *(const Raw<C> *)(base + p.at[i] + voff);
+            for (int i = 0; i < LOADS; ++i) f[i] = *(const Raw<C> *)(from + p.at[i] + voff);
         } else {
             const int n = hi - t0;
-            const auto res = make_rsrc(base + (n > 0 ? (seq_row0 + t0) * stride : 0) + (int64_t)kvh * RB,
+            const auto res = make_rsrc(from + (n > 0 ? (seq_row0 + t0) * stride : 0) + (int64_t)kvh * RB,
                                        n > 0 ? (uint32_t)(min(n, tile) - 1) * (uint32_t)stride + RB : 0u);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) f[i] = load_piece<C>(res, voff + (uint32_t)((NW * i + wave) * RPL) * (uint32_t)stride);
@@ -171,7 +176,7 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
         const int i = min(i0 + lane, a.n_seqs - 1);
         const int c0 = a.cu[i], c1 = a.cu[i + 1];
         const int keys = prompt_keys(a, i), rows = (c1 - c0) * a.group;
-        const PromptCut cut = prompt_cut(rows, keys, a.kv_heads);
+        const PromptCut cut = prompt_cut(rows, keys, a.kv_heads, a.prompt_grid);
         const bool in = i0 + lane < a.n_seqs;
         const int x = wave_scan(in ? (rows + ROWS - 1) / ROWS * cut.parts : 0);
         const int y = wave_scan(in && cut.parts > 1 ? rows * a.kv_heads * cut.parts : 0);
@@ -280,10 +285,9 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     const int32_t *table_row = PAGED ? a.kv.table + (int64_t)t.seq * a.kv.max_blocks : nullptr;
     const int64_t seq_row0 = PAGED ? 0 : t.tok0;
     const int lrow = lane / L::PPR, lp = lane % L::PPR;
-    const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
-    const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
     using Loads = KvLoads<C, PAGED, NW, L::RPL, LOADS, RB>;
-    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}};
+    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}, 0, 0};
+    const uint32_t kvoff = ld.voff(lrow, a.kv.k_stride, lp * CB), vvoff = ld.voff(lrow, a.kv.v_stride, lp * CB);
     struct Flight {
         Raw<C> k[LOADS], v[LOADS];
         typename Loads::Place p;
@@ -292,9 +296,8 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         ld.place(a.kv, t0, &f.p);
         ld.load(f.k, a.kv.k, f.p, a.kv.k_stride, kvoff, t0, KT);
         ld.load(f.v, a.kv.v, f.p, a.kv.v_stride, vvoff, t0, KT);
-        ld.look(a.kv, t0 + KT);
     };
-    ld.look(a.kv, t.lo);
+    ld.begin(a.kv, t.lo);
     load(t.lo, f0);
     load(t.lo + KT, f1);
 

@@ -56,11 +56,9 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     const int32_t *table_row = PAGED ? a.kv.table + (int64_t)t.seq * a.kv.max_blocks : nullptr;
     const int64_t seq_row0 = PAGED ? 0 : t.tok0;
     const int lrow = lane / PPR, lp = lane % PPR;
-    const uint32_t kvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.k_stride) + lp * CB);
-    const uint32_t vvoff = (uint32_t)(lrow * (PAGED ? RB : (int)a.kv.v_stride) + lp * CB);
-
     using Loads = KvLoads<C, PAGED, 4, RPL, LOADS, RB>;
-    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}};
+    Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}, 0, 0};
+    const uint32_t kvoff = ld.voff(lrow, a.kv.k_stride, lp * CB), vvoff = ld.voff(lrow, a.kv.v_stride, lp * CB);
     typename Loads::Place kplace, vplace;
     Raw<C> fk[LOADS], fv[LOADS];
     // A turn's loads: keys of the tile at t0, values of the tile before it.
@@ -69,12 +67,10 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
         ld.load(fv, a.kv.v, vplace, a.kv.v_stride, vvoff, t0 - KT, KT);
         ld.place(a.kv, t0, &kplace);
         ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t0, KT);
-        ld.look(a.kv, t0 + KT);
     };
-    ld.look(a.kv, t.lo);
+    ld.begin(a.kv, t.lo);
     ld.place(a.kv, t.lo, &kplace);
     ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t.lo, KT);
-    ld.look(a.kv, t.lo + KT);
 
     const int row = t.row0 + 32 * wave + col;
     const bool live = row < t.n_rows;
