@@ -442,9 +442,11 @@ la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const i
  * it does not see have no effect on it, infinities and NaN included (one
  * exception: an infinite value with a weight that rounds to zero gives
  * infinity or NaN).  Scores, maxima and sums are fp32; with bf16 inputs the
- * weights p_j are rounded to bf16 for the product with v.  Results do not
- * depend on the other sequences of a call: how a row's keys are cut into
- * tiles and parts follows from its own sequence (and group) alone.
+ * weights p_j are rounded to bf16 for the product with v.  The same call
+ * gives the same bits.  A single token's result does not depend on the other
+ * sequences of its call (its group's prefix apart); a prompt's keys are summed
+ * in parts where the whole call has few rows, so its last bits may differ
+ * between a small and a large batch.
  * --------------------------------------------------------------------- */
 
 /* Shape of an attention call.  Strides are elements from one token to the

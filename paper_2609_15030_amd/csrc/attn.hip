@@ -107,41 +107,69 @@ la::KvSource cached(const la_kv_layer *y) {
 
 // --- prompts -----------------------------------------------------------------
 
+// Workgroups of a split call, at most: two on every CU; fp32, whose products take
+// eight times as long and whose partial sums so weigh less, eight.  (256 tokens at
+// 3,328 x 8 heads: 84 us whole, 24 split; three fp32 prompts of 1,791, 640 and 257:
+// 98 whole, 65 split.)
+constexpr int64_t prompt_grid(bool f32) { return f32 ? 2048 : 512; }
+
 struct PromptPlan {
     int64_t tokens = 0, items = 0;      // items: row tiles times parts, of one key head
     int64_t slots = 0, joins = 0;       // (row, part) results in the workspace; workgroups that join them
     int32_t max_kv = 0;
-    bool wide = false;                  // bf16: attn_wide_kernel; fp32: attn_prompt_kernel of `waves` waves
-    int waves = 8;
+    int part_shift = 0;                 // keys of a part, as a power of two; 0: rows are not split
+    bool ordered = false;
+    uint8_t order[64];                  // sequences, the longest first
 };
+
+// Waves of an fp32 workgroup, 16 rows each (eight took 74 us where four take 65:
+// three ragged prompts).
+constexpr int kF32Waves = 4;
 
 la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *kv_len, PromptPlan *p) {
     if (!cu) return fail(LA_ERR_INVALID_ARG, "cu_seqlens_host is required");
     if (cu[0] != 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens[0]=%d", cu[0]);
     const int64_t group = s->q_heads / s->kv_heads;
-    int64_t items4 = 0;
+    const bool f32 = s->io_dtype == LA_F32;
+    auto keys_of = [&](int i) { return kv_len ? kv_len[i] : cu[i + 1] - cu[i]; };
+    auto tiles = [&](int rows, int shift) {
+        int64_t n = 0;
+        for (int i = 0; i < s->n_seqs; ++i) n += up((cu[i + 1] - cu[i]) * group, rows) * la::prompt_parts(keys_of(i), shift);
+        return n;
+    };
     for (int i = 0; i < s->n_seqs; ++i) {
         const int64_t n = (int64_t)cu[i + 1] - cu[i];
         if (n < 0) return fail(LA_ERR_INVALID_ARG, "cu_seqlens decreases at sequence %d", i);
         if (n * group > 0x7fffff00) return fail(LA_ERR_INVALID_ARG, "sequence %d is too long for one launch", i);
-        const int32_t keys = kv_len ? kv_len[i] : (int32_t)n;
-        if (keys < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys);
-        p->max_kv = std::max(p->max_kv, keys);
-        const int parts = la::prompt_cut((int)(n * group), keys, s->kv_heads, la::prompt_grid(s->io_dtype == LA_F32)).parts;
-        p->items += up(n * group, la::kPromptRows) * parts;
-        items4 += up(n * group, la::kPromptRows / 2) * parts;
-        if (parts > 1 && n > 0) {
-            p->slots += n * s->q_heads * parts;
-            p->joins += up(n * s->q_heads, 1024 / s->head_dim);
-        }
+        if (keys_of(i) < 0) return fail(LA_ERR_INVALID_ARG, "kv_len[%d]=%d", i, keys_of(i));
+        p->max_kv = std::max(p->max_kv, keys_of(i));
     }
     p->tokens = cu[s->n_seqs];
-    p->wide = s->io_dtype == LA_BF16;
-    // fp32: 64 rows a workgroup while 128 would leave CUs idle
-    if (!p->wide && p->items * s->kv_heads < 256) {
-        p->waves = 4;
-        p->items = items4;
+    const int tile = f32 ? 16 * kF32Waves : la::kPromptRows;
+    p->items = tiles(tile, 0);
+    // two parts save less than joining them costs (512 tokens x 8 heads: 16.7 us whole, 18 in two)
+    if (p->items * s->kv_heads <= prompt_grid(f32) / 2 && p->max_kv > 2 << la::kPromptPartShift)
+        for (int shift = la::kPromptPartShift; (1 << shift) < p->max_kv; ++shift) {
+            const int64_t n = tiles(tile, shift);
+            if (n * s->kv_heads > prompt_grid(f32)) continue;
+            p->part_shift = shift;
+            p->items = n;
+            break;
+        }
+    // A long sequence's tiles that begin late are what a large call ends on (16 prompts
+    // with suffixes of 80 to 8,064 tokens: 727 us in the caller's order).
+    if (!p->part_shift && s->n_seqs > 1 && s->n_seqs <= 64 && p->items * s->kv_heads > prompt_grid(f32)) {
+        p->ordered = true;
+        for (int i = 0; i < s->n_seqs; ++i) p->order[i] = (uint8_t)i;
+        std::stable_sort(p->order, p->order + s->n_seqs, [&](int x, int y) { return keys_of(x) > keys_of(y); });
     }
+    if (p->part_shift)
+        for (int i = 0; i < s->n_seqs; ++i) {
+            const int64_t rows = (int64_t)(cu[i + 1] - cu[i]) * s->q_heads, parts = la::prompt_parts(keys_of(i), p->part_shift);
+            if (parts == 1) continue;
+            p->slots += rows * parts;
+            p->joins += up(rows, 1024 / s->head_dim);
+        }
     if (p->items * s->kv_heads > kMaxGrid || p->slots > kMaxGrid)
         return fail(LA_ERR_INVALID_ARG, "too many row tiles for one launch");
     return LA_OK;
@@ -159,8 +187,7 @@ la_status launch_prompt(const la::AttnArgs &a, const PromptPlan &p, hipStream_t 
     const dim3 grid((unsigned)(p.items * a.kv_heads));
     if constexpr (sizeof(T) == 2)
         hipLaunchKernelGGL((la::attn_wide_kernel<C, D, PAGED>), grid, dim3(la::kWideThreads), 0, st, a);
-    else if (p.waves == 4) hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 4>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, 8>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, kF32Waves>), grid, dim3(64 * kF32Waves), 0, st, a);
     if (la_status e = hip_check("attention prompt launch")) return e;
     if (p.joins == 0) return LA_OK;
     hipLaunchKernelGGL((la::attn_join_prompt_kernel<T, D>), dim3((unsigned)p.joins), dim3(256), 0, st, a);
@@ -184,7 +211,9 @@ la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer 
     a.by_kv_heads = la::FastDiv::by((uint32_t)a.kv_heads);
     a.n_seqs = s->n_seqs;
     a.max_kv = p.max_kv;
-    a.prompt_grid = la::prompt_grid(s->io_dtype == LA_F32);
+    a.part_shift = p.part_shift;
+    a.ordered = p.ordered;
+    if (p.ordered) std::copy(p.order, p.order + 64, a.order);
     carve_parts(&a, ws, p.slots, s->head_dim);
     (void)hipGetLastError();
     const int d = s->head_dim;

@@ -66,12 +66,14 @@ struct AttnArgs {
     float c, v_scale;              // scale * k_scale * log2(e); value of a stored v of 1
     int32_t n_seqs, kv_heads, group, n_groups;
     FastDiv by_group, by_kv_heads; // row / group, item / kv_heads
-    uint32_t prompt_grid;          // prompts: see prompt_cut
+    int32_t part_shift;            // prompts: keys of a part, as a power of two; 0: whole rows
     int32_t max_kv;                // longest kv_len that the tables and the workspace cover
     int32_t parts;                 // decode: parts the workspace holds for each row
     int32_t prefix_parts;          // decode: of these, the most of a prefix
     int32_t group_tiles;           // decode: row tiles of the largest group
     int32_t prefix_items;          // decode: workgroups of the prefixes, ahead of the others
+    bool ordered;                  // prompts: sequences in `order` (up to 64), the longest first
+    uint8_t order[64];
     bool direct;                   // decode: one part each, written straight to o
     float *part_o;                 // [slot][D]
     float2 *part_ml;               // [slot]
@@ -81,26 +83,15 @@ struct AttnArgs {
 constexpr int kPrefixPart = 256;
 constexpr int kOwnPart = 256;
 
-// A prompt's keys are cut into parts where its rows alone would leave much of the
-// chip idle: as many as make prompt_grid workgroups of 128 rows with the
-// sequence's own row tiles, of at least kPromptPart keys.  The rule looks at one
-// sequence only, so its bits do not depend on the batch.
+// Prompts: rows of a tile in bf16.  Where a call's row tiles alone would leave much
+// of the chip idle, every sequence's keys are cut into parts of 2^part_shift (0: not
+// cut), the smallest power of two from 2^kPromptPartShift on that makes no more than
+// prompt_grid workgroups.
 constexpr int kPromptRows = 128;
-constexpr int kPromptPart = 256;
-__host__ __device__ inline uint32_t prompt_grid(bool f32) { return f32 ? 1024 : 256; }
+constexpr int kPromptPartShift = 8;
 
-// Keys of a part (a multiple of 64) and parts of a sequence of `rows` rows under
-// each key head that reads `keys` keys.
-struct PromptCut {
-    int part, parts;
-};
-__host__ __device__ inline PromptCut prompt_cut(int rows, int keys, int kv_heads, uint32_t grid) {
-    const uint32_t tiles = (uint32_t)(rows + kPromptRows - 1) / kPromptRows * (uint32_t)kv_heads;
-    const uint32_t most = (uint32_t)(keys + kPromptPart - 1) / kPromptPart;
-    if (tiles == 0 || tiles > grid / 2 || most < 2) return {keys, 1};
-    const uint32_t fill = grid / tiles, parts = fill < most ? fill : most;
-    const uint32_t part = (((uint32_t)keys + parts - 1) / parts + 63) & ~63u;
-    return {(int)part, (int)(((uint32_t)keys + part - 1) / part)};
+__host__ __device__ inline int prompt_parts(int keys, int part_shift) {
+    return part_shift && keys > (1 << part_shift) ? (int)(((uint32_t)keys + (1u << part_shift) - 1) >> part_shift) : 1;
 }
 
 // --- 16-byte pieces of rows, as the LDS tiles hold them ---------------------

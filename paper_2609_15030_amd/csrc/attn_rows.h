@@ -326,13 +326,13 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
     constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 4;
     const int heads = a.kv_heads * a.group, wl = threadIdx.x & 63;
     int before = 0, slots = 0, seq = -1, local = 0, c0 = 0, new_tokens = 0, keys = 0;
-    PromptCut cut{0, 1};
+    int stride = 1;
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
         const int i = min(i0 + wl, a.n_seqs - 1);
         const int b0 = a.cu[i], n = a.cu[i + 1] - b0, k = prompt_keys(a, i);
-        const PromptCut pc = prompt_cut(n * a.group, k, a.kv_heads, a.prompt_grid);
-        const bool in = i0 + wl < a.n_seqs && pc.parts > 1;
-        const int x = wave_scan(in ? (n * heads + ROWS - 1) / ROWS : 0), y = wave_scan(in ? n * heads * pc.parts : 0);
+        const int parts = prompt_parts(k, a.part_shift);
+        const bool in = i0 + wl < a.n_seqs && parts > 1;
+        const int x = wave_scan(in ? (n * heads + ROWS - 1) / ROWS : 0), y = wave_scan(in ? n * heads * parts : 0);
         const uint64_t past = __ballot(before + x > (int)blockIdx.x);
         if (!past) {
             before += __builtin_amdgcn_readlane(x, 63);
@@ -346,14 +346,14 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
         c0 = __builtin_amdgcn_readlane(b0, at);
         new_tokens = __builtin_amdgcn_readlane(n, at);
         keys = __builtin_amdgcn_readlane(k, at);
-        cut = {__builtin_amdgcn_readlane(pc.part, at), __builtin_amdgcn_readlane(pc.parts, at)};
+        stride = __builtin_amdgcn_readlane(parts, at);
         break;
     }
     if (seq < 0) return;
     const int lane = threadIdx.x % LANES, row = local * ROWS + threadIdx.x / LANES;
     if (row >= new_tokens * heads) return;
     const int tok = a.by_group(a.by_kv_heads(row)), head = row - tok * heads;
-    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + cut.part - 1) / cut.part, stride = cut.parts;
+    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + (1 << a.part_shift) - 1) >> a.part_shift;
     const int64_t slot = slots + (int64_t)row * stride;
     const float2 *ml = a.part_ml + slot;
     const float *po = a.part_o + slot * D + 4 * lane;

@@ -173,13 +173,13 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     t->prefix = false;
     int before = 0, slots = 0;
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-        const int i = min(i0 + lane, a.n_seqs - 1);
+        const int i = a.ordered ? a.order[min(lane, a.n_seqs - 1)] : min(i0 + lane, a.n_seqs - 1);
         const int c0 = a.cu[i], c1 = a.cu[i + 1];
         const int keys = prompt_keys(a, i), rows = (c1 - c0) * a.group;
-        const PromptCut cut = prompt_cut(rows, keys, a.kv_heads, a.prompt_grid);
+        const int parts = prompt_parts(keys, a.part_shift);
         const bool in = i0 + lane < a.n_seqs;
-        const int x = wave_scan(in ? (rows + ROWS - 1) / ROWS * cut.parts : 0);
-        const int y = wave_scan(in && cut.parts > 1 ? rows * a.kv_heads * cut.parts : 0);
+        const int x = wave_scan(in ? (rows + ROWS - 1) / ROWS * parts : 0);
+        const int y = wave_scan(in && parts > 1 ? rows * a.kv_heads * parts : 0);
         const uint64_t past = __ballot(before + x > r);
         if (!past) {
             before += __builtin_amdgcn_readlane(x, 63);
@@ -189,12 +189,11 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
         const int at = __builtin_ctzll(past);
         const int local = r - before - (at ? __builtin_amdgcn_readlane(x, at - 1) : 0);
         t->slot0 = slots + (at ? __builtin_amdgcn_readlane(y, at - 1) : 0);
-        t->seq = i0 + at;
+        t->seq = __builtin_amdgcn_readlane(i, at);
         t->tok0 = __builtin_amdgcn_readlane(c0, at);
         t->n_rows = __builtin_amdgcn_readlane(rows, at);
         t->keys = __builtin_amdgcn_readlane(keys, at);
-        t->n_parts = t->slot_parts = __builtin_amdgcn_readlane(cut.parts, at);
-        const int pt = __builtin_amdgcn_readlane(cut.part, at);
+        t->n_parts = t->slot_parts = __builtin_amdgcn_readlane(parts, at);
         const int tiles = (t->n_rows + ROWS - 1) / ROWS;
         t->part = 0;
         int tile = local;
@@ -208,8 +207,8 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
         t->hi = row_limit(a, *t, min(t->row0 + ROWS, t->n_rows) - 1);
         t->lo = 0;
         if (t->n_parts > 1) {
-            t->lo = t->part * pt;
-            t->hi = min(t->hi, t->lo + pt);
+            t->lo = t->part << a.part_shift;
+            t->hi = min(t->hi, t->lo + (1 << a.part_shift));
             return t->lo < t->hi;
         }
         return true;

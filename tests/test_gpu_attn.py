@@ -268,22 +268,41 @@ def test_single_tokens(case):
 
 # --- what a call may not depend on ---------------------------------------------
 
-def test_a_sequence_does_not_depend_on_its_batch():
-    case = ([70, 256, 33], [700, 600, 33], 8, 2, 128, "bf16", "bf16", 16)
-    q, cache = _resume(case, 41)
-    whole = api.AttnPrefill(8, 2, 128, case[0], case[1]).run_paged(cache.layer(), q).clone()
-    at = 0
-    for i, (n, L) in enumerate(zip(case[0], case[1])):
-        one = la.make_kv_layer(cache.dev, cache.table_dev[i:i + 1], 16, 2, 128, torch.bfloat16, *cache.off)
-        o = api.AttnPrefill(8, 2, 128, [n], [L]).run_paged(one, q[at:at + n])
-        assert torch.equal(o, whole[at:at + n])
-        at += n
-    kv = torch.tensor(case[1], dtype=torch.int32, device="cuda")
-    qd = q[:3].contiguous()
-    batch = api.AttnDecode(3, 8, 2, 128, 700).run(cache.layer(), qd, kv).clone()
+def test_a_single_token_does_not_depend_on_its_batch():
+    gen = torch.Generator().manual_seed(41)
+    kv = [700, 600, 33]
+    cache = Cache(gen, kv, 2, 128, "bf16", 16)
+    q = _rand(gen, 3, 8, 128).to(torch.bfloat16).cuda()
+    kv_dev = torch.tensor(kv, dtype=torch.int32, device="cuda")
+    batch = api.AttnDecode(3, 8, 2, 128, 700).run(cache.layer(), q, kv_dev).clone()
     for i in range(3):
         one = la.make_kv_layer(cache.dev, cache.table_dev[i:i + 1], 16, 2, 128, torch.bfloat16, *cache.off)
-        assert torch.equal(api.AttnDecode(1, 8, 2, 128, 700).run(one, qd[i:i + 1], kv[i:i + 1].clone()), batch[i:i + 1])
+        assert torch.equal(api.AttnDecode(1, 8, 2, 128, 700).run(one, q[i:i + 1], kv_dev[i:i + 1].clone()), batch[i:i + 1])
+
+
+@pytest.mark.parametrize("io,kind", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_a_batch_of_every_length(io, kind):
+    """70 sequences (more than one step of the item search), from none to many parts: a
+    small call that splits its keys and a large one that takes sequences longest first
+    give what the oracle does; each twice the same bits."""
+    rng = np.random.default_rng(46)
+    for n_seqs, rows, most in ((70, 3, 900), (12, 400, 2000)):
+        new = [int(x) for x in rng.integers(0, rows + 1, n_seqs)]
+        kv = [n + int(x) for n, x in zip(new, rng.integers(0, most, n_seqs))]
+        case = (new, kv, 4, 2, 64, io, kind, 16)
+        q, cache = _resume(case, 47)
+        plan = api.AttnPrefill(4, 2, 64, new, kv, TYPES[io])
+        o = plan.run_paged(cache.layer(), q).clone()
+        torch.cuda.synchronize()
+        assert torch.equal(plan.run_paged(cache.layer(), q), o)
+        some = range(n_seqs) if rows < 10 else (0, 3, 7, 11)         # the oracle is slow: a few of the long ones
+        ref, at = [], 0
+        for i, (n, L) in enumerate(zip(new, kv)):
+            if i in some:
+                k, v = cache.rows(i)
+                ref.append((at, oa.attend(_host(q[at:at + n]), k, v, L - n, 0.125), max(L, 1)))
+            at += n
+        _check(o, ref, 64, io == "bf16", f"{n_seqs} sequences, {kind}")
 
 
 def test_missing_blocks_are_counted_and_read_as_zero():
