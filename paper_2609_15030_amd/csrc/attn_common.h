@@ -129,24 +129,30 @@ template <typename C> __device__ inline uint4 piece_of(const Raw<C> &p) {
     }
 }
 
-// Infinities and NaN of a piece made zero; true if there was one.
-template <typename T> __device__ inline bool drop_nonfinite(uint4 &x) {
+// Whether a piece holds an infinity or NaN (an exponent of all ones).  bf16: both
+// exponents of a word at once, a one added to each carries into the sign's place.
+template <typename T> __device__ inline bool has_nonfinite(const uint4 &x) {
+    if constexpr (sizeof(T) == 2) {
+        constexpr uint32_t E = 0x7F807F80u, ONE = 0x00800080u;
+        return ((((x.x & E) + ONE) | ((x.y & E) + ONE) | ((x.z & E) + ONE) | ((x.w & E) + ONE)) & 0x80008000u) != 0;
+    } else {
+        constexpr uint32_t E = 0x7F800000u;
+        return (x.x & E) == E || (x.y & E) == E || (x.z & E) == E || (x.w & E) == E;
+    }
+}
+
+// Those made zero.
+template <typename T> __device__ inline void drop_nonfinite(uint4 &x) {
     uint32_t *w = &x.x;
-    bool any = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (sizeof(T) == 2) {
-            const bool lo = (w[i] & 0x7F80u) == 0x7F80u, hi = (w[i] & 0x7F800000u) == 0x7F800000u;
-            if (lo) w[i] &= 0xFFFF0000u;
-            if (hi) w[i] &= 0x0000FFFFu;
-            any |= lo | hi;
+            if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
+            if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0x0000FFFFu;
         } else {
-            const bool bad = (w[i] & 0x7F800000u) == 0x7F800000u;
-            if (bad) w[i] = 0;
-            any |= bad;
+            if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] = 0;
         }
     }
-    return any;
 }
 
 // Byte offsets of runs of 16 cached tokens behind a layer's keys (and values), for

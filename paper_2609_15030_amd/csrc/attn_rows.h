@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_decode_kernel(AttnArgs a
 // lanes a row, 1,024 / D rows a workgroup.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
-    constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 4;
+    constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
     const int heads = a.kv_heads * a.group, wl = threadIdx.x & 63;
     int before = 0, slots = 0, seq = -1, local = 0, c0 = 0, new_tokens = 0, keys = 0;
     int stride = 1;

@@ -261,6 +261,7 @@ template <typename T, int D, int NW> struct TileLds {
         };
         float out[NW][16][D + 4];                // results on their way out; the padding puts 16 rows on different banks
     };
+    int64_t where[NW][16];                       // and where their rows go, in elements (-1: nowhere)
     int dropped;
 };
 
@@ -324,7 +325,10 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
             const int at = ((NW * i + wave) * L::RPL + lrow) * L::PS + lp;
             sm.k[b][at] = Loads::piece(f.k[i], f.p, i);
             uint4 v = Loads::piece(f.v[i], f.p, i);
-            if (mixed && drop_nonfinite<T>(v)) sm.dropped = 1;
+            if (mixed && has_nonfinite<T>(v)) {
+                drop_nonfinite<T>(v);
+                sm.dropped = 1;
+            }
             sm.v[b][at] = v;
         }
     };
@@ -427,9 +431,17 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     // Results go out as whole rows, through LDS (the last barrier is behind every read of its tiles).
     const bool whole = t.n_parts == 1;
     const float x = whole ? row_scale(a, l) : 1.f;
-    const int heads = a.kv_heads * a.group;
-    if (!whole && live && limit > t.lo && g == 0)
-        a.part_ml[t.slot0 + ((tok - t.tok0) * heads + head) * t.slot_parts + t.part] = make_float2(m, l);
+    if (g == 0) {
+        int64_t at = -1;
+        if (live && whole) {
+            at = tok * a.o_stride + (int64_t)head * D;
+        } else if (live && limit > t.lo) {
+            const int64_t slot = t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
+            a.part_ml[slot] = make_float2(m, l);
+            at = slot * D;
+        }
+        sm.where[wave][col] = at;
+    }
 #pragma unroll
     for (int d = 0; d < DT; ++d) *(f32x4 *)&sm.out[wave][col][16 * d + 4 * g] = acc[d] * x;
     constexpr int RL = D / 4, RS = 64 / RL;      // lanes a row, rows a step
@@ -437,12 +449,10 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     for (int r0 = 0; r0 < 16; r0 += RS) {
         const int r = r0 + lane / RL, e = lane % RL * 4;
         const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
-        const int rr = t.row0 + 16 * wave + r;
-        if (rr >= t.n_rows) continue;
-        const int rt = a.by_group(rr), rh = t.kvh * a.group + rr - rt * a.group;
-        if (whole) store4((T *)a.o + (t.tok0 + rt) * a.o_stride + (int64_t)rh * D + e, y);
-        else if (row_limit(a, t, rr) > t.lo)
-            store4(a.part_o + (t.slot0 + ((int64_t)rt * heads + rh) * t.slot_parts + t.part) * D + e, y);
+        const int64_t at = sm.where[wave][r];
+        if (at < 0) continue;
+        if (whole) store4((T *)a.o + at + e, y);
+        else store4(a.part_o + at + e, y);
     }
 }
 

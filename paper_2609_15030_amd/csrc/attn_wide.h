@@ -36,6 +36,7 @@ template <int D> struct WideLds {
         };
         float out[4][32][D + 4];                 // results on their way out; the padding puts 8 rows on different banks
     };
+    int64_t where[4][32];                        // and where their rows go, in elements (-1: nowhere)
     int dropped;
 };
 
@@ -95,7 +96,10 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             uint4 v = Loads::piece(fv[i], vplace, i);
-            if (mixed && drop_nonfinite<__bf16>(v)) sm.dropped = 1;
+            if (mixed && has_nonfinite<__bf16>(v)) {
+                drop_nonfinite<__bf16>(v);
+                sm.dropped = 1;
+            }
             sm.v[b][((4 * i + wave) * RPL + lrow) * L::VS + lp] = v;
         }
     };
@@ -117,9 +121,9 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     // weights of the 32 keys from t0 on; returns what the row's sums so far shrink by
     auto weights = [&](int t0, bool masked, f32x16 &s, bf16x8 (&p)[2]) {
         if (masked) {
+            const int seen = edge - t0 - 4 * hf;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (t0 + 8 * (i >> 2) + 4 * hf + (i & 3) >= edge) s[i] = -INFINITY;
+            for (int i = 0; i < 16; ++i) s[i] = seen > 8 * (i >> 2) + (i & 3) ? s[i] : -INFINITY;
         }
         float top = fmaxf(s[0], s[1]);
 #pragma unroll
@@ -217,8 +221,17 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     // there of one row, and storing those as they are took as long as two turns.
     const bool whole = t.n_parts == 1;
     const float x = whole ? row_scale(a, l) : 1.f;
-    const int64_t slot = whole ? 0 : t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
-    if (!whole && live && limit > t.lo && hf == 0) a.part_ml[slot] = make_float2(m, l);
+    if (hf == 0) {
+        int64_t at = -1;
+        if (live && whole) {
+            at = tok * a.o_stride + (int64_t)head * D;
+        } else if (live && limit > t.lo) {
+            const int64_t slot = t.slot0 + ((tok - t.tok0) * (a.kv_heads * a.group) + head) * t.slot_parts + t.part;
+            a.part_ml[slot] = make_float2(m, l);
+            at = slot * D;
+        }
+        sm.where[wave][col] = at;
+    }
 #pragma unroll
     for (int d = 0; d < MT32; ++d)
 #pragma unroll
@@ -226,18 +239,23 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
             *(f32x4 *)&sm.out[wave][col][32 * d + 8 * q + 4 * hf] =
                 f32x4{acc[d][4 * q], acc[d][4 * q + 1], acc[d][4 * q + 2], acc[d][4 * q + 3]} * x;
     // rows of this wave only: its LDS operations are in order
-    constexpr int RL = D / 4, RS = 64 / RL;      // lanes a row, rows a step
+    if (whole) {
+        constexpr int RL = D / 8, RS = 64 / RL;  // lanes a row, rows a step
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += RS) {
-        const int r = r0 + lane / RL, e = lane % RL * 4;
-        const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
-        const int rr = t.row0 + 32 * wave + r, seen = __shfl(limit, r);
-        if (rr >= t.n_rows) continue;
-        const int rt = a.by_group(rr), rh = t.kvh * a.group + rr - rt * a.group;
-        if (whole) {
-            store4((__bf16 *)a.o + (t.tok0 + rt) * a.o_stride + (int64_t)rh * D + e, y);
-        } else if (seen > t.lo) {
-            store4(a.part_o + (t.slot0 + ((int64_t)rt * (a.kv_heads * a.group) + rh) * t.slot_parts + t.part) * D + e, y);
+        for (int r0 = 0; r0 < 32; r0 += RS) {
+            const int r = r0 + lane / RL, e = lane % RL * 8;
+            const f32x4 y0 = *(const f32x4 *)&sm.out[wave][r][e], y1 = *(const f32x4 *)&sm.out[wave][r][e + 4];
+            const int64_t at = sm.where[wave][r];
+            if (at >= 0) *(bf16x8 *)((__bf16 *)a.o + at + e) = pack8(y0, y1);
+        }
+    } else {
+        constexpr int RL = D / 4, RS = 64 / RL;
+#pragma unroll 4
+        for (int r0 = 0; r0 < 32; r0 += RS) {
+            const int r = r0 + lane / RL, e = lane % RL * 4;
+            const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
+            const int64_t at = sm.where[wave][r];
+            if (at >= 0) store4(a.part_o + at + e, y);
         }
     }
 }
