@@ -201,9 +201,11 @@ def _hptr(a, dtype) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
+    """The hipStream_t of a torch stream, a handle, or (None) torch's current
+    stream.  The last by its raw handle: torch.cuda.current_stream() makes a
+    Python object of it, which takes 2.5 of the 13 us of a short decode call."""
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -455,19 +457,22 @@ def la_hybrid_restore(kv: LaKvBlocks, boundary_dev, boundary_host, state_pool, s
 # ---------------------------------------------------------------------------
 
 _DTYPES = {torch.bfloat16: LA_BF16, torch.float32: LA_F32, torch.float8_e4m3fn: LA_FP8_E4M3}
+_TORCH = {v: k for k, v in _DTYPES.items()}
 _I32 = torch.int32
 
 
-def _rows_ptr(t, heads: int, dim: int) -> int:
-    """Device pointer of a [tokens, heads, dim] tensor whose heads are packed
-    within a token (a slice of a wider projection will do)."""
-    if not t.is_cuda:
-        raise ValueError("expected a device tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"expected [tokens, {heads}, {dim}], got {tuple(t.shape)}")
-    if not t.is_contiguous() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+def _rows(t, dtype, shape):
+    """(device pointer, elements from one token to the next) of a [tokens, heads,
+    dim] tensor whose heads are packed within a token (a slice of a wider
+    projection will do); 0 stands for packed tokens."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError(f"expected a {dtype} device tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    n, heads, dim = shape
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
         raise ValueError("expected packed heads within a token")
-    return t.data_ptr()
+    return t.data_ptr(), t.stride(0) if n > 1 else 0
 
 
 def _dtype_of(dtype) -> int:
@@ -477,16 +482,11 @@ def _dtype_of(dtype) -> int:
     return d
 
 
-def _token_stride(t) -> int:
-    """Elements from one token to the next (0, packed, for packed rows or one token)."""
-    return 0 if t.is_contiguous() or t.shape[0] == 1 else t.stride(0)
-
-
 def _ids(t, what) -> Optional[int]:
     """Device pointer of an int32 tensor."""
     if t is None:
         return None
-    if t.dtype != _I32 or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous int32 device tensor")
     return t.data_ptr()
 
@@ -546,22 +546,12 @@ def make_block_pool(cache, block_tokens: int, table, ref_count, free_list, free_
     return p
 
 
-def _with_strides(shape: LaAttnShape, q, k, v, o):
-    """The shape with these tensors' token strides: itself, or a copy where they differ."""
-    qs, os_ = _token_stride(q), _token_stride(o)
-    ks, vs = (0, 0) if k is None else (_token_stride(k), _token_stride(v))
-    if shape.q_stride != qs or shape.o_stride != os_ or shape.k_stride != ks or shape.v_stride != vs:
+def _with_strides(shape: LaAttnShape, qs: int, ks: int, vs: int, os_: int):
+    """The shape with these token strides: itself, or a copy where they differ."""
+    if shape.q_stride != qs or shape.k_stride != ks or shape.v_stride != vs or shape.o_stride != os_:
         shape = LaAttnShape.from_buffer_copy(shape)
         shape.q_stride, shape.k_stride, shape.v_stride, shape.o_stride = qs, ks, vs, os_
     return ctypes.byref(shape)
-
-
-def _attn_io(shape: LaAttnShape, q, o, rows):
-    if _dtype_of(q.dtype) != shape.io_dtype or o.dtype != q.dtype:
-        raise ValueError("q and o must have the shape's io_dtype")
-    if q.shape[0] != rows or o.shape[0] != rows:
-        raise ValueError(f"q and o must have {rows} rows")
-    return _rows_ptr(q, shape.q_heads, shape.head_dim), _rows_ptr(o, shape.q_heads, shape.head_dim)
 
 
 def _ws(workspace):
@@ -576,14 +566,12 @@ def la_attn_prefill_workspace_bytes(shape: LaAttnShape, cu_host: np.ndarray, kv_
 def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o, workspace=None, stream=None,
                     check: bool = True) -> int:
     """q, o [T, q_heads, d], k, v [T, kv_heads, d]: heads packed, tokens at any stride."""
-    T = int(cu_host[shape.n_seqs])
-    qp, op = _attn_io(shape, q, o, T)
-    if k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != T or v.shape[0] != T:
-        raise ValueError(f"k and v must have q's type and {T} rows")
-    H, d = shape.kv_heads, shape.head_dim
+    T, dt = int(cu_host[shape.n_seqs]), _TORCH[shape.io_dtype]
+    rows, kv = (T, shape.q_heads, shape.head_dim), (T, shape.kv_heads, shape.head_dim)
+    (qp, qs), (kp, ks), (vp, vs), (op, os_) = _rows(q, dt, rows), _rows(k, dt, kv), _rows(v, dt, kv), _rows(o, dt, rows)
     w, n = _ws(workspace)
-    st = _lib.la_attn_prefill(_with_strides(shape, q, k, v, o), qp, _rows_ptr(k, H, d), _rows_ptr(v, H, d),
-                              _ids(cu_dev, "cu_seqlens"), _hptr(cu_host, np.int32), op, w, n, _stream(stream))
+    st = _lib.la_attn_prefill(_with_strides(shape, qs, ks, vs, os_), qp, kp, vp, _ids(cu_dev, "cu_seqlens"),
+                              _hptr(cu_host, np.int32), op, w, n, _stream(stream))
     if check:
         _check(st)
     return st
@@ -591,11 +579,12 @@ def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o,
 
 def la_attn_prefill_paged(shape: LaAttnShape, layer: LaKvLayer, q, cu_dev, cu_host: np.ndarray, kv_len_dev,
                           kv_len_host: np.ndarray, o, workspace=None, stream=None, check: bool = True) -> int:
-    qp, op = _attn_io(shape, q, o, int(cu_host[shape.n_seqs]))
+    rows, dt = (int(cu_host[shape.n_seqs]), shape.q_heads, shape.head_dim), _TORCH[shape.io_dtype]
+    (qp, qs), (op, os_) = _rows(q, dt, rows), _rows(o, dt, rows)
     if layer._seqs < shape.n_seqs:
         raise ValueError("the block table has fewer rows than the call sequences")
     w, n = _ws(workspace)
-    st = _lib.la_attn_prefill_paged(_with_strides(shape, q, None, None, o), ctypes.byref(layer), qp,
+    st = _lib.la_attn_prefill_paged(_with_strides(shape, qs, 0, 0, os_), ctypes.byref(layer), qp,
                                     _ids(cu_dev, "cu_seqlens"), _hptr(cu_host, np.int32),
                                     _ids(kv_len_dev, "kv_len"), _hptr(kv_len_host, np.int32), op, w, n,
                                     _stream(stream))
@@ -610,13 +599,14 @@ def la_attn_decode_workspace_bytes(shape: LaAttnShape, max_kv_len: int, max_pref
 
 def la_attn_decode(shape: LaAttnShape, layer: LaKvLayer, q, kv_len_dev, max_kv_len: int, o,
                    groups: Optional[LaPrefixGroups] = None, workspace=None, stream=None, check: bool = True) -> int:
-    qp, op = _attn_io(shape, q, o, shape.n_seqs)
-    if layer._seqs < shape.n_seqs or kv_len_dev.numel() < shape.n_seqs:
+    n_seqs = shape.n_seqs
+    rows, dt = (n_seqs, shape.q_heads, shape.head_dim), _TORCH[shape.io_dtype]
+    (qp, qs), (op, os_) = _rows(q, dt, rows), _rows(o, dt, rows)
+    if layer._seqs < n_seqs or kv_len_dev.numel() < n_seqs:
         raise ValueError("the block table or kv_len has fewer rows than the call sequences")
     w, n = _ws(workspace)
-    st = _lib.la_attn_decode(_with_strides(shape, q, None, None, o), ctypes.byref(layer), qp,
-                             _ids(kv_len_dev, "kv_len"), int(max_kv_len),
-                             None if groups is None else ctypes.byref(groups), op, w, n, _stream(stream))
+    st = _lib.la_attn_decode(_with_strides(shape, qs, 0, 0, os_), ctypes.byref(layer), qp, _ids(kv_len_dev, "kv_len"),
+                             max_kv_len, None if groups is None else ctypes.byref(groups), op, w, n, _stream(stream))
     if check:
         _check(st)
     return st
@@ -624,14 +614,12 @@ def la_attn_decode(shape: LaAttnShape, layer: LaKvLayer, q, kv_len_dev, max_kv_l
 
 def la_kv_write(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: bool = True) -> int:
     """k, v [T, kv_heads, d] into the cache blocks of the sequences of cu_dev [n_seqs + 1]."""
-    n_seqs = cu_dev.numel() - 1
-    if k.dtype != v.dtype or k.shape != v.shape:
-        raise ValueError("k and v must have one type and shape")
+    n_seqs, dt = cu_dev.numel() - 1, k.dtype
     if layer._seqs < n_seqs or kv_len_dev.numel() < n_seqs:
         raise ValueError("the block table or kv_len has fewer rows than the call sequences")
-    H, d = layer.kv_heads, layer.head_dim
-    st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(k.dtype), _rows_ptr(k, H, d), _token_stride(k), _rows_ptr(v, H, d),
-                          _token_stride(v), _ids(cu_dev, "cu_seqlens"), n_seqs, k.shape[0],
+    kv = (k.shape[0], layer.kv_heads, layer.head_dim)
+    (kp, ks), (vp, vs) = _rows(k, dt, kv), _rows(v, dt, kv)
+    st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(dt), kp, ks, vp, vs, _ids(cu_dev, "cu_seqlens"), n_seqs, kv[0],
                           _ids(kv_len_dev, "kv_len"), _stream(stream))
     if check:
         _check(st)
@@ -639,9 +627,11 @@ def la_kv_write(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: 
 
 
 def _same_count(*lists):
-    if len({t.numel() for t in lists}) != 1:
-        raise ValueError("lists of one length are expected")
-    return lists[0].numel()
+    n = lists[0].numel()
+    for t in lists[1:]:
+        if t.numel() != n:
+            raise ValueError("lists of one length are expected")
+    return n
 
 
 def la_blocks_copy(pool: LaBlockPool, src_ids, dst_ids, stream=None, check: bool = True) -> int:
