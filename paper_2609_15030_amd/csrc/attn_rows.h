@@ -184,8 +184,11 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < VL; ++i) {
-                    uint4 *const to = (uint4 *)vt + (16 * n + VR * i + lane / VPR) * PS;
-                    const uint4 x = f.v[n][i];
+                    const int row = 16 * n + VR * i + lane / VPR;
+                    uint4 *const to = (uint4 *)vt + row * PS;
+                    uint4 x = f.v[n][i];
+                    // keys that the prefix's part has: a weight of zero would not undo an infinity
+                    if (t0 < first && t0 + row < first) x = make_uint4(0, 0, 0, 0);
                     if constexpr (F8) {
                         const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
                         to[2 * (lane % VPR)] = make_uint4(e0.x, e0.y, e1.x, e1.y);

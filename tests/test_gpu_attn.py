@@ -305,6 +305,30 @@ def test_a_batch_of_every_length(io, kind):
         _check(o, ref, 64, io == "bf16", f"{n_seqs} sequences, {kind}")
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_infinities_beside_the_end_of_a_prefix(io):
+    """A prefix of 37 keys ends inside a run of 16: its last values and the first own
+    ones, infinite or NaN, reach the column they stand in and no other."""
+    gen = torch.Generator().manual_seed(48)
+    kv = [90, 61, 37]
+    cache = Cache(gen, kv, 2, 64, io, 16, shared=[(0, 3, 37)])
+    q = _rand(gen, 3, 4, 64).to(TYPES[io]).cuda()
+    kv_dev, cu, pre = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (kv, [0, 3], [37]))
+    plan = api.AttnDecode(3, 4, 2, 64, 90, TYPES[io], cu_group=cu, max_prefix_len=37)
+    clean = plan.run(cache.layer(), q, kv_dev, pre).clone()
+    v = cache.part(cache.dev, 1)
+    at = int(cache.table[0, 2])
+    v[at, :, 34 - 32, 3] = float("inf")
+    v[at, :, 36 - 32, 5] = float("nan")
+    v[at, :, 37 - 32, 7] = -float("inf")             # the first own key of two of them; none of the third
+    o = plan.run(cache.layer(), q, kv_dev, pre)
+    torch.cuda.synchronize()
+    assert torch.isposinf(o[:, :, 3]).all() and torch.isnan(o[:, :, 5]).all()
+    assert torch.isneginf(o[:2, :, 7]).all() and torch.equal(o[2, :, 7], clean[2, :, 7])
+    rest = [i for i in range(64) if i not in (3, 5, 7)]
+    assert torch.equal(o[:, :, rest], clean[:, :, rest])
+
+
 def test_missing_blocks_are_counted_and_read_as_zero():
     case = ([40], [200], 4, 2, 128, "bf16", "bf16", 16)
     q, cache = _resume(case, 42)
