@@ -558,9 +558,13 @@ la_status la_blocks_compact(const la_block_pool *pool, int32_t *new_ids_dev, voi
     if (copy_blocks + table_blocks + a.n_chunks > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "the table is too large for one launch");
     hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(la::compact_count_kernel, dim3((unsigned)a.n_chunks), dim3(la::kBlockThreads), 0, st, a);
-    if (la_status e = hip_check("compaction launch")) return e;
-    hipLaunchKernelGGL(la::compact_rank_kernel, dim3((unsigned)a.n_chunks), dim3(la::kBlockThreads), 0, st, a);
+    if (a.n_chunks <= la::kCompactSmall) {
+        hipLaunchKernelGGL(la::compact_rank_kernel<true>, dim3((unsigned)a.n_chunks), dim3(la::kBlockThreads), 0, st, a);
+    } else {
+        hipLaunchKernelGGL(la::compact_count_kernel, dim3((unsigned)a.n_chunks), dim3(la::kBlockThreads), 0, st, a);
+        if (la_status e = hip_check("compaction launch")) return e;
+        hipLaunchKernelGGL(la::compact_rank_kernel<false>, dim3((unsigned)a.n_chunks), dim3(la::kBlockThreads), 0, st, a);
+    }
     if (la_status e = hip_check("compaction launch")) return e;
     hipLaunchKernelGGL(la::compact_move_kernel, dim3((unsigned)(copy_blocks + table_blocks + a.n_chunks)), dim3(la::kBlockThreads), 0, st, a,
                        (int32_t)copy_blocks, (int32_t)parts, (int32_t)table_blocks);

@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kBlockThreads) void extend_kernel(BlockPoolArgs p, 
         const int64_t first = e0 + threadIdx.x * E;
         int32_t *at[E];
         int want = 0, total;
-        int i = first < all ? (int)(first / p.max_blocks) : n;
+        int i = first >= all ? n : first >> 32 ? (int)(first / p.max_blocks) : (int)((uint32_t)first / (uint32_t)p.max_blocks);
         int64_t j = first - i * p.max_blocks;
         int row = i < n ? rows[i] : -1, tokens = i < n ? len[i] : 0;
 #pragma unroll
@@ -232,23 +232,39 @@ __global__ __launch_bounds__(256) void free_rows_kernel(BlockPoolArgs p, const i
     }
 }
 
-// One workgroup: the marked blocks go on the stack, ids ascending.
+// One workgroup: the marked blocks go on the stack, ids ascending.  A wave takes
+// an equal share of up to 16,384 ids, 64 at a time.
 __global__ __launch_bounds__(kBlockThreads) void free_push_kernel(BlockPoolArgs p) {
     constexpr int E = 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int at = *p.free_count;
-    for (int64_t b0 = 0; b0 < p.n_blocks; b0 += kBlockThreads * E) {
-        const int64_t first = b0 + threadIdx.x * E;
+    const int steps = (int)min((int64_t)E, (p.n_blocks + kBlockThreads - 1) / kBlockThreads);
+    for (int64_t b0 = 0; b0 < p.n_blocks; b0 += kBlockThreads * steps) {
+        const int64_t first = b0 + wave * (64 * steps) + lane;
         uint32_t marked = 0;
         int total;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (first + e < p.n_blocks && p.ref[first + e] == kFreed) marked |= 1u << e;
-        int k = at + block_sum_before(__popc(marked), &total);
-        for (; marked; marked &= marked - 1) {
-            const int64_t id = first + __ffs(marked) - 1;
+        for (int e = 0; e < E; ++e) {
+            if (e >= steps) break;
+            const int64_t id = min(first + 64 * e, p.n_blocks - 1);
+            if (p.ref[id] == kFreed && first + 64 * e < p.n_blocks) marked |= 1u << e;
+        }
+        int mine = 0;                              // of the wave: all, and those before this lane's e-th
+        int before[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (e >= steps) break;
+            const uint64_t here = __ballot(marked >> e & 1);
+            before[e] = mine + __popcll(here & ((1ull << lane) - 1));
+            mine += __popcll(here);
+        }
+        const int k = at + __builtin_amdgcn_readfirstlane(block_sum_before(lane == 0 ? mine : 0, &total));
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (!(marked >> e & 1)) continue;
+            const int64_t id = first + 64 * e;
             p.ref[id] = 0;
-            if (k < p.n_blocks) p.free_list[k] = (int32_t)id;
-            ++k;
+            if (k + before[e] < p.n_blocks) p.free_list[k + before[e]] = (int32_t)id;
         }
         at += total;
     }
@@ -283,19 +299,34 @@ __device__ inline int counts_before(const CompactArgs &a, int to) {
 }
 
 // With n live blocks: the k-th live id at or past n goes to the k-th free id
-// below n.  Each workgroup ranks 1,024 ids.
+// below n.  Each workgroup ranks 1,024 ids.  SMALL (up to kCompactSmall chunks):
+// each counts the whole pool itself, so that no launch has to do it before.
+constexpr int kCompactSmall = 32;
+template <bool SMALL>
 __global__ __launch_bounds__(kBlockThreads) void compact_rank_kernel(CompactArgs a) {
     const BlockPoolArgs &p = a.p;
-    const int n = counts_before(a, a.n_chunks);
-    const int below = counts_before(a, blockIdx.x);
-    // live ids below n: whole chunks, then the chunk that n falls into
-    const int cn = n / kBlockThreads;
-    int in_chunk;
-    {
+    int n, below, stay;
+    if constexpr (SMALL) {
+        uint32_t live = 0;                         // bit c: id 1,024 c + thread
+#pragma unroll 8
+        for (int c = 0; c < a.n_chunks; ++c) {
+            const int id = c * kBlockThreads + threadIdx.x;
+            if (p.ref[min((int64_t)id, p.n_blocks - 1)] > 0 && id < p.n_blocks) live |= 1u << c;
+        }
+        block_sum_before(__popc(live), &n);
+        block_sum_before(__popc(live & ((1u << blockIdx.x) - 1)), &below);
+        const int whole = n / kBlockThreads + ((int)threadIdx.x < n % kBlockThreads);      // of this thread's ids, those below n
+        block_sum_before(__popc(whole < 32 ? live & ((1u << whole) - 1) : live), &stay);
+    } else {
+        n = counts_before(a, a.n_chunks);
+        below = counts_before(a, blockIdx.x);
+        // live ids below n: whole chunks, then the chunk that n falls into
+        const int cn = n / kBlockThreads;
+        int in_chunk;
         const int64_t id = (int64_t)cn * kBlockThreads + threadIdx.x;
         block_sum_before(id < n && id < p.n_blocks && p.ref[id] > 0, &in_chunk);
+        stay = counts_before(a, cn) + in_chunk;
     }
-    const int stay = counts_before(a, cn) + in_chunk;
     const int64_t id = (int64_t)blockIdx.x * kBlockThreads + threadIdx.x;
     const bool live = id < p.n_blocks && p.ref[id] > 0;
     int total;

@@ -139,6 +139,20 @@ def test_many_blocks_and_rows():
     p.compact()
 
 
+def test_a_pool_of_many_small_blocks():
+    """More ids than a workgroup counts by itself."""
+    width, rows = 1100, 20
+    p = Pair(33000, 16, 1, rows, width)
+    p.extend(list(range(rows)), [width - 7 * i for i in range(rows)])
+    p.free([2, 19, 7, 7])
+    p.extend([7], [width])
+    p.free([r for r in range(rows) if r not in (0, 5, 7)])
+    p.compact()
+    p.fork([0, 5], [1, 2], [1000, 40])
+    p.free([0])
+    p.compact()
+
+
 def test_blocks_past_32_bit_offsets():
     pool = api.BlockPool.new(4200, 1 << 20, 16, 2, 2)
     pool.cache[4199] = 7
