@@ -457,7 +457,7 @@ typedef struct la_attn_shape {
     int32_t q_heads, kv_heads;       /* q_heads a multiple of kv_heads             */
     int32_t head_dim;                /* built: 64, 128                             */
     int32_t io_dtype;                /* LA_BF16 or LA_F32: q, k, v, o              */
-    float scale;                     /* > 0                                        */
+    float scale;                     /* > 0; times k_scale a normal fp32           */
     int64_t q_stride, k_stride, v_stride, o_stride;
 } la_attn_shape;
 

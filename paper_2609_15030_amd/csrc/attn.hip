@@ -42,6 +42,15 @@ la_status check_attn_shape(const la_attn_shape *s) {
     return LA_OK;
 }
 
+// What a score is multiplied by to become a base-2 exponent.  Masked scores are
+// minus infinity when they are multiplied, so it may not have become zero.
+la_status exponent_scale(const la_attn_shape *s, float k_scale, float *out) {
+    *out = s->scale * k_scale * la::kAttnLog2e;
+    if (!std::isnormal(*out))
+        return fail(LA_ERR_INVALID_ARG, "scale=%g times k_scale=%g is out of fp32's range", (double)s->scale, (double)k_scale);
+    return LA_OK;
+}
+
 // A token stride in elements: 0 stands for packed rows.
 la_status token_stride(int64_t given, int64_t heads, const la_attn_shape *s, const char *what, int64_t *out) {
     const int64_t packed = heads * s->head_dim;
@@ -67,7 +76,7 @@ la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
     if (y->n_blocks < 1 || y->n_blocks > 0x7fffffff) return fail(LA_ERR_INVALID_ARG, "n_blocks=%lld", (long long)y->n_blocks);
     const int64_t part = (int64_t)y->kv_heads * bt * y->head_dim * dtype_size(y->dtype);
     if (y->block_bytes < 0 || y->block_bytes % 16 || y->k_offset < 0 || y->v_offset < 0 || y->k_offset % 16 || y->v_offset % 16 ||
-        y->k_offset + part > y->block_bytes || y->v_offset + part > y->block_bytes)
+        y->k_offset > y->block_bytes - part || y->v_offset > y->block_bytes - part)
         return fail(LA_ERR_INVALID_ARG, "keys at %lld and values at %lld (%lld bytes each) must lie in a block of %lld bytes, on 16-byte lines",
                     (long long)y->k_offset, (long long)y->v_offset, (long long)part, (long long)y->block_bytes);
     if (y->k_offset < y->v_offset + part && y->v_offset < y->k_offset + part)
@@ -347,7 +356,7 @@ la_status la_attn_prefill(const la_attn_shape *shape, const void *q, const void 
     a.kv.k_stride = ks * dtype_size(shape->io_dtype);
     a.kv.v_stride = vs * dtype_size(shape->io_dtype);
     a.cu = cu_seqlens_dev;
-    a.c = shape->scale * la::kAttnLog2e;
+    if (la_status e = exponent_scale(shape, 1.f, &a.c)) return e;
     a.v_scale = 1.f;
     return run_prompt(shape, a, nullptr, p, workspace, ws_bytes, (hipStream_t)stream);
 }
@@ -370,7 +379,7 @@ la_status la_attn_prefill_paged(const la_attn_shape *shape, const la_kv_layer *l
     a.kv = cached(layer);
     a.cu = cu_seqlens_dev;
     a.kv_len = kv_len_dev;
-    a.c = shape->scale * layer->k_scale * la::kAttnLog2e;
+    if (la_status e = exponent_scale(shape, layer->k_scale, &a.c)) return e;
     a.v_scale = layer->v_scale;
     return run_prompt(shape, a, layer, p, workspace, ws_bytes, (hipStream_t)stream);
 }
@@ -409,7 +418,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     if (need && !aligned16(workspace)) return fail(LA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     a.kv = cached(layer);
     a.kv_len = kv_len_dev;
-    a.c = shape->scale * layer->k_scale * la::kAttnLog2e;
+    if (la_status e = exponent_scale(shape, layer->k_scale, &a.c)) return e;
     a.v_scale = layer->v_scale;
     a.n_seqs = shape->n_seqs;
     a.kv_heads = shape->kv_heads;

@@ -182,3 +182,16 @@ def test_binding_refuses_wrong_tensors():
         la._dtype_of(torch.float16)
     with pytest.raises(ValueError):
         la._ids(table.long(), "table")
+
+
+def test_factors_out_of_range_are_refused():
+    """Sizes and factors each fine by itself whose sum or product is not."""
+    assert _prefill(_shape(scale=1e-39)) == la.LA_ERR_INVALID_ARG               # a subnormal exponent factor
+    s, tiny = _shape(scale=1e-20), _layer(dtype=la.LA_FP8_E4M3, k_scale=1e-20)
+    assert _paged(s, tiny) == la.LA_ERR_INVALID_ARG and _decode(s, tiny) == la.LA_ERR_INVALID_ARG
+    s, vast = _shape(scale=1e30), _layer(dtype=la.LA_FP8_E4M3, k_scale=1e30)
+    assert _paged(s, vast) == la.LA_ERR_INVALID_ARG and _decode(s, vast) == la.LA_ERR_INVALID_ARG
+    for name in ("k_offset", "v_offset"):                                       # past the end by more than an int64 holds
+        y = _layer(**{name: (1 << 63) - 16})
+        assert _paged(_shape(), y) == la.LA_ERR_INVALID_ARG
+        assert LIB.la_kv_write(ctypes.byref(y), la.LA_BF16, P, 0, P, 0, P, 2, 10, P, None) == la.LA_ERR_INVALID_ARG
