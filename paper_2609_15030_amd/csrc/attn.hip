@@ -118,8 +118,8 @@ la::KvSource cached(const la_kv_layer *y) {
 
 // Workgroups of a split call, at most: two on every CU; fp32, whose products take
 // eight times as long and whose partial sums so weigh less, eight.  (256 tokens at
-// 3,328 x 8 heads: 84 us whole, 24 split; three fp32 prompts of 1,791, 640 and 257:
-// 98 whole, 65 split.)
+// 3,328 x 8 heads: 77 us whole, 23 split; three fp32 prompts of 1,791, 640 and 257:
+// 101 whole, 61 split.)
 constexpr int64_t prompt_grid(bool f32) { return f32 ? 2048 : 512; }
 
 struct PromptPlan {
@@ -130,10 +130,6 @@ struct PromptPlan {
     bool ordered = false;
     uint8_t order[64];                  // sequences, the longest first
 };
-
-// Waves of an fp32 workgroup, 16 rows each (eight took 74 us where four take 65:
-// three ragged prompts).
-constexpr int kF32Waves = 4;
 
 la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *kv_len, PromptPlan *p) {
     if (!cu) return fail(LA_ERR_INVALID_ARG, "cu_seqlens_host is required");
@@ -154,9 +150,9 @@ la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *
         p->max_kv = std::max(p->max_kv, keys_of(i));
     }
     p->tokens = cu[s->n_seqs];
-    const int tile = f32 ? 16 * kF32Waves : la::kPromptRows;
+    const int tile = f32 ? la::kTileRows : la::kPromptRows;
     p->items = tiles(tile, 0);
-    // two parts save less than joining them costs (512 tokens x 8 heads: 16.7 us whole, 18 in two)
+    // two parts save no more than joining them costs (512 tokens x 8 heads: 15.5 us whole, 15.7 in two)
     if (p->items * s->kv_heads <= prompt_grid(f32) / 2 && p->max_kv > 2 << la::kPromptPartShift)
         for (int shift = la::kPromptPartShift; (1 << shift) < p->max_kv; ++shift) {
             const int64_t n = tiles(tile, shift);
@@ -166,7 +162,7 @@ la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *
             break;
         }
     // A long sequence's tiles that begin late are what a large call ends on (16 prompts
-    // with suffixes of 80 to 8,064 tokens: 727 us in the caller's order).
+    // with suffixes of 80 to 8,064 tokens: 615 us, 700 in the caller's order).
     if (!p->part_shift && s->n_seqs > 1 && s->n_seqs <= 64 && p->items * s->kv_heads > prompt_grid(f32)) {
         p->ordered = true;
         for (int i = 0; i < s->n_seqs; ++i) p->order[i] = (uint8_t)i;
@@ -196,7 +192,7 @@ la_status launch_prompt(const la::AttnArgs &a, const PromptPlan &p, hipStream_t 
     const dim3 grid((unsigned)(p.items * a.kv_heads));
     if constexpr (sizeof(T) == 2)
         hipLaunchKernelGGL((la::attn_wide_kernel<C, D, PAGED>), grid, dim3(la::kWideThreads), 0, st, a);
-    else hipLaunchKernelGGL((la::attn_prompt_kernel<T, C, D, PAGED, kF32Waves>), grid, dim3(64 * kF32Waves), 0, st, a);
+    else hipLaunchKernelGGL((la::attn_tile_kernel<D, PAGED>), grid, dim3(la::kTileThreads), 0, st, a);
     if (la_status e = hip_check("attention prompt launch")) return e;
     if (p.joins == 0) return LA_OK;
     hipLaunchKernelGGL((la::attn_join_prompt_kernel<T, D>), dim3((unsigned)p.joins), dim3(256), 0, st, a);
@@ -434,7 +430,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
         a.prefix_len = groups->prefix_len_dev;
         a.n_groups = groups->n_groups;
         a.prefix_parts = p.prefix_parts;
-        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, shape->io_dtype == LA_F32 ? 16 * la::kDecodeWaves : la::kPromptRows);
+        a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, shape->io_dtype == LA_F32 ? la::kTileRows : la::kPromptRows);
         prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups * a.kv_heads;
     }
     if (items > kMaxGrid || rows > kMaxGrid || prefix_items + kRowsGrid > kMaxGrid)

@@ -20,7 +20,7 @@ constexpr int kRowsHeads = 16;
 
 template <typename T, int D> struct RowsLds {
     static constexpr int KT = sizeof(T) == 2 ? 32 : 16;       // keys of a wave's tile
-    static constexpr int PS = AttnTile<T, D>::PS;
+    static constexpr int PS = D * (int)sizeof(T) / 16 + 1;    // 16-byte pieces of a row in LDS, one of them padding
     union {
         uint4 v[kDecodeWaves][KT * PS];
         float sum[kDecodeWaves][kRowsHeads][D];
@@ -307,16 +307,17 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
 template <typename T, typename C, int D>
 __global__ __launch_bounds__(kRowsThreads, 2) void attn_decode_kernel(AttnArgs a) {
     constexpr bool WIDE = sizeof(T) == 2;
-    constexpr int ROWS = WIDE ? kPromptRows : 16 * kDecodeWaves;
+    constexpr int ROWS = WIDE ? kPromptRows : kTileRows;
+    static_assert(kRowsThreads == kWideThreads && kRowsThreads == kTileThreads, "one launch for both");
     __shared__ union Lds {
-        std::conditional_t<WIDE, WideLds<D>, TileLds<T, D, kDecodeWaves>> tile;
+        std::conditional_t<WIDE, WideLds<D>, TileLds<D>> tile;
         RowsLds<T, D> rows;
     } sm;
     if ((int)blockIdx.x < a.prefix_items) {
         RowTile t;
         if (!prefix_tile_of<ROWS>(a, blockIdx.x, &t)) return;
         if constexpr (WIDE) wide_run<C, D, true>(a, t, sm.tile);
-        else tile_run<T, C, D, true, kDecodeWaves>(a, t, sm.tile);
+        else tile_run<D, true>(a, t, sm.tile);
     } else {
         rows_run<T, C, D>(a, (int)blockIdx.x - a.prefix_items, (int)gridDim.x - a.prefix_items, sm.rows);
     }

@@ -1,29 +1,13 @@
-// Attention of tiles of rows, 16 for each wave, over key tiles in LDS: prompts of
-// few rows, fp32 prompts, and the shared prefix of a decode group (rows: the
-// group's sequences; every row reads the same keys).
-//
-// Key tiles are double buffered, and two more are in flight in registers, so that
-// a tile's loads have two tiles' time to arrive: a workgroup's tile takes about a
-// microsecond and memory about as long to answer.
+// What the kernels over tiles of rows share (their work, their loads), and fp32
+// attention of such tiles: four waves of 16 rows over key tiles in LDS.  Prompts,
+// and the shared prefix of a decode group (rows: the group's sequences; every row
+// reads the same keys).
 #pragma once
 #include "attn_common.h"
 
 namespace la {
 
-// Key tile of the kernel and one tile of rows in LDS: 16-byte pieces, one piece of
-// padding behind each row.  With it the 16 rows of one piece (a K fragment) fall
-// on different banks, the 16 rows x 32 bytes (bf16) that a V fragment's transposed
-// reads take at once on every bank twice, and the 4 rows x 64 bytes (fp32) on
-// different banks; and a lane's addresses differ by constants, which an
-// exclusive-or of row and piece would not give (it took 40 more registers).
-template <typename T, int D> struct AttnTile {
-    static constexpr int N = Piece<T>::N, PPR = D / N, PS = PPR + 1;
-    static constexpr int KT = sizeof(T) == 2 || D == 64 ? 64 : 32;
-    static constexpr int RPL = 64 / PPR;                  // rows that a wave loads at once
-    static constexpr int PIECES = KT * PS;
-};
-
-// A workgroup's loads of key tiles (of 64 keys, or 32): wave w of NW takes runs of
+// A workgroup's loads of key tiles: wave w of NW takes runs of
 // RPL rows, run i at rows (NW i + w) RPL of the tile.
 //
 // Packed rows: one resource from the tile's first row to the last key; rows past
@@ -253,26 +237,37 @@ __device__ inline void add_nonfinite(const AttnArgs &a, const int32_t *table_row
     }
 }
 
-// LDS of a workgroup of NW waves.
-template <typename T, int D, int NW> struct TileLds {
+// fp32: key tiles of 32 keys, double buffered, and two more in flight in registers,
+// so that a tile's loads have two tiles' time to arrive.  Bound by the matrix unit
+// where a call fills the chip (8,192 tokens x 8 heads x 64: 101 TFLOP/s of the 154
+// that a large product reaches), by the uneven tiles of its parts where it does
+// not (1,791 + 640 + 257 tokens: 61 us, 62 TFLOP/s).  At 32 keys and 64 dims four
+// workgroups share a CU; at 64 keys two did (66 us).
+//
+// LDS: 16-byte pieces, one piece of padding behind each row.  With it the 16 rows
+// of one piece (a K fragment) fall on different banks, and so do the 4 rows x 64
+// bytes of a V fragment; and a lane's addresses differ by constants, which an
+// exclusive-or of row and piece would not give (it took 40 more registers).
+constexpr int kTileWaves = 4, kTileRows = 16 * kTileWaves, kTileThreads = 64 * kTileWaves;
+
+template <int D> struct TileLds {
+    static constexpr int KT = 32, PPR = D / 4, PS = PPR + 1;
     union {
         struct {
-            uint4 k[2][AttnTile<T, D>::PIECES], v[2][AttnTile<T, D>::PIECES];
+            uint4 k[2][KT * PS], v[2][KT * PS];
         };
-        float out[NW][16][D + 4];                // results on their way out; the padding puts 16 rows on different banks
+        float out[kTileWaves][16][D + 4];        // results on their way out; the padding puts 16 rows on different banks
     };
-    int64_t where[NW][16];                       // and where their rows go, in elements (-1: nowhere)
+    int64_t where[kTileWaves][16];               // and where their rows go, in elements (-1: nowhere)
     int dropped;
 };
 
-template <typename T, typename C, int D, bool PAGED, int NW>
-__device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, TileLds<T, D, NW> &sm) {
-    using L = AttnTile<T, D>;
-    using M = MT<T>;
-    constexpr int KT = L::KT, NT = KT / 16, DT = D / 16, LOADS = KT / (NW * L::RPL);
-    constexpr int NQ = sizeof(T) == 2 ? D / 32 : D / 16;       // 16-byte pieces of a q row for each lane
-    constexpr int CB = Piece<T>::N * sizeof(C), RB = D * sizeof(C);    // stored bytes of a piece, of a row
-    static_assert(LOADS >= 1 && LOADS * NW * L::RPL == KT, "key tile");
+template <int D, bool PAGED>
+__device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, TileLds<D> &sm) {
+    using L = TileLds<D>;
+    constexpr int KT = L::KT, NT = KT / 16, DT = D / 16, NQ = D / 16;          // NQ: 16-byte pieces of a q row for each lane
+    constexpr int RPL = 64 / L::PPR, LOADS = KT / (kTileWaves * RPL), RB = D * sizeof(float);
+    static_assert(LOADS >= 1 && LOADS * kTileWaves * RPL == KT, "key tile");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -285,11 +280,11 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
     const int32_t *table_row = PAGED ? a.kv.table + (int64_t)t.seq * a.kv.max_blocks : nullptr;
     const int64_t seq_row0 = PAGED ? 0 : t.tok0;
     const int lrow = lane / L::PPR, lp = lane % L::PPR;
-    using Loads = KvLoads<C, PAGED, NW, L::RPL, LOADS, RB>;
+    using Loads = KvLoads<float, PAGED, kTileWaves, RPL, LOADS, RB>;
     Loads ld{table_row, seq_row0, t.kvh, t.hi, wave, {}, 0, 0};
-    const uint32_t kvoff = ld.voff(lrow, a.kv.k_stride, lp * CB), vvoff = ld.voff(lrow, a.kv.v_stride, lp * CB);
+    const uint32_t kvoff = ld.voff(lrow, a.kv.k_stride, 16 * lp), vvoff = ld.voff(lrow, a.kv.v_stride, 16 * lp);
     struct Flight {
-        Raw<C> k[LOADS], v[LOADS];
+        Raw<float> k[LOADS], v[LOADS];
         typename Loads::Place p;
     } f0, f1;
     auto load = [&](int t0, Flight &f) {
@@ -303,12 +298,9 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
 
     uint4 qf[NQ];
     {
-        const T *qp = (const T *)a.q + tok * a.q_stride + (int64_t)head * D;
+        const float *qp = (const float *)a.q + tok * a.q_stride + (int64_t)head * D + 4 * g;
 #pragma unroll
-        for (int s = 0; s < NQ; ++s) {
-            const int p = 4 * s + g;                            // bf16: dims 32 s + 8 g ..; fp32: 16 s + 4 g ..
-            qf[s] = live ? *(const uint4 *)(qp + p * Piece<T>::N) : make_uint4(0, 0, 0, 0);
-        }
+        for (int s = 0; s < NQ; ++s) qf[s] = live ? *(const uint4 *)(qp + 16 * s) : make_uint4(0, 0, 0, 0);
     }
     const int all_see = t.all_see;
     int wave_hi = limit;                         // the most keys that a row of the wave sees
@@ -322,11 +314,11 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         const bool mixed = t0 + KT > all_see;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = ((NW * i + wave) * L::RPL + lrow) * L::PS + lp;
+            const int at = ((kTileWaves * i + wave) * RPL + lrow) * L::PS + lp;
             sm.k[b][at] = Loads::piece(f.k[i], f.p, i);
             uint4 v = Loads::piece(f.v[i], f.p, i);
-            if (mixed && has_nonfinite<T>(v)) {
-                drop_nonfinite<T>(v);
+            if (mixed && has_nonfinite<float>(v)) {
+                drop_nonfinite<float>(v);
                 sm.dropped = 1;
             }
             sm.v[b][at] = v;
@@ -346,13 +338,9 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
 #pragma unroll
             for (int k = 0; k < NQ; ++k) {
                 const uint4 kf = sm.k[b][(16 * n + col) * L::PS + 4 * k + g];
-                if constexpr (sizeof(T) == 2) {
-                    s[n] = M::mma(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), s[n]);
-                } else {
-                    const float *x = (const float *)&kf, *y = (const float *)&qf[k];
+                const float *x = (const float *)&kf, *y = (const float *)&qf[k];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[n] = M::mma(x[e], y[e], s[n]);
-                }
+                for (int e = 0; e < 4; ++e) s[n] = MT<float>::mma(x[e], y[e], s[n]);
             }
         }
         const bool masked = t0 + KT > all_see;
@@ -382,28 +370,14 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[d][i] *= shrink;
-        const char *vt = (const char *)sm.v[b];
-        if constexpr (sizeof(T) == 2) {
-            const char *at = vt + (4 * g + (col >> 2)) * L::PS * 16 + 8 * (col & 3);
+        const char *at = (const char *)sm.v[b] + 4 * g * L::PS * 16 + 4 * col;
 #pragma unroll
-            for (int k = 0; k < NT / 2; ++k) {
-                const bf16x8 p = pack8(s[2 * k], s[2 * k + 1]);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const char *x = at + 32 * k * L::PS * 16 + 32 * d;
-                    acc[d] = M::mma(join_tr(lds_tr(x), lds_tr(x + 16 * L::PS * 16)), p, acc[d]);
-                }
-            }
-        } else {
-            const char *at = vt + 4 * g * L::PS * 16 + 4 * col;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        acc[d] = M::mma(*(const float *)(at + (16 * n + i) * L::PS * 16 + 64 * d), s[n][i], acc[d]);
-        }
+                for (int d = 0; d < DT; ++d)
+                    acc[d] = MT<float>::mma(*(const float *)(at + (16 * n + i) * L::PS * 16 + 64 * d), s[n][i], acc[d]);
     };
     // Two tiles a turn, so that the register sets and buffers are constants; the
     // loads run past the last tile (as zeros) rather than being skipped, since a
@@ -426,7 +400,7 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         const int first = all_see <= t.lo ? t.lo : t.lo + (all_see - t.lo) / KT * KT;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            add_nonfinite<C, D, PAGED>(a, table_row, seq_row0, t.kvh, first, t.hi, limit, 16 * d + 4 * g, acc[d]);
+            add_nonfinite<float, D, PAGED>(a, table_row, seq_row0, t.kvh, first, t.hi, limit, 16 * d + 4 * g, acc[d]);
     }
     // Results go out as whole rows, through LDS (the last barrier is behind every read of its tiles).
     const bool whole = t.n_parts == 1;
@@ -451,16 +425,15 @@ __device__ __forceinline__ void tile_run(const AttnArgs &a, const RowTile &t, Ti
         const f32x4 y = *(const f32x4 *)&sm.out[wave][r][e];
         const int64_t at = sm.where[wave][r];
         if (at < 0) continue;
-        if (whole) store4((T *)a.o + at + e, y);
-        else store4(a.part_o + at + e, y);
+        store4((whole ? (float *)a.o : a.part_o) + at + e, y);
     }
 }
 
-template <typename T, typename C, int D, bool PAGED, int NW>
-__global__ __launch_bounds__(64 * NW) void attn_prompt_kernel(AttnArgs a) {
-    __shared__ TileLds<T, D, NW> sm;
+template <int D, bool PAGED>
+__global__ __launch_bounds__(kTileThreads) void attn_tile_kernel(AttnArgs a) {
+    __shared__ TileLds<D> sm;
     RowTile t;
-    if (prompt_tile_of<16 * NW>(a, blockIdx.x, &t)) tile_run<T, C, D, PAGED, NW>(a, t, sm);
+    if (prompt_tile_of<kTileRows>(a, blockIdx.x, &t)) tile_run<D, PAGED>(a, t, sm);
 }
 
 }  // namespace la
