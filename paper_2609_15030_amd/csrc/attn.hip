@@ -535,7 +535,8 @@ la_status la_blocks_free(const la_block_pool *pool, const int32_t *rows_dev, int
     (void)hipGetLastError();
     hipLaunchKernelGGL(la::free_rows_kernel, dim3((unsigned)up(p.max_blocks, 256), (unsigned)n), dim3(256), 0, st, p, rows_dev);
     if (la_status e = hip_check("free launch")) return e;
-    hipLaunchKernelGGL(la::free_push_kernel, dim3(1), dim3(la::kBlockThreads), 0, st, p);
+    hipLaunchKernelGGL(p.n_blocks <= la::kPushSmall ? la::free_push_kernel<4> : la::free_push_kernel<16>, dim3(1),
+                       dim3(la::kBlockThreads), 0, st, p);
     return hip_check("free launch");
 }
 

@@ -1,6 +1,17 @@
 // The blocks of an attention cache: new keys and values written into them, and
 // their bookkeeping (copy, fork, extend, free, compact) on the device.
 //
+// Bytes: a copied or moved block is read and written once (a fork copies only a
+// last block that its tokens end inside); beside that 4 bytes for each table entry
+// and block id.  Copies run at the rate of a large copy (5.0 TB/s) once they are
+// many; small calls are bound by their launches and by chains of loads (row ->
+// table entry -> id), which is why a call is few kernels and each thread's loads
+// are independent.  Measured, in us: 64 forks of 517 to 3,584 tokens with their 64
+// children freed 16.2 (fork_take 2.9, fork 6.5, free_rows 3, free_push 2.6); 16
+// rows of 17 to 3,328 tokens with four freed, compacted and grown
+// again 49.5 (rank 4.9, move 28 at 4.9 TB/s, extend 6, free 6).  Freeing in one workgroup
+// instead of two kernels took 9 to 25: one CU's atomics are too slow.
+//
 // Block ids live in a table [rows, max_blocks] (-1: none); ref[b] counts the
 // entries that name b; the free ids are a stack, the next one at its top.
 // Everything that hands out or takes back several blocks does so in a fixed
@@ -233,27 +244,26 @@ __global__ __launch_bounds__(256) void free_rows_kernel(BlockPoolArgs p, const i
 }
 
 // One workgroup: the marked blocks go on the stack, ids ascending.  A wave takes
-// an equal share of up to 16,384 ids, 64 at a time.
+// 64 E ids at a time, 64 side by side.  E = 16 for large pools, whose passes are a
+// chain; E = 4 up to kPushSmall ids, which are one pass (2.6 us where 16 take 4.4).
+constexpr int kPushSmall = 4 * kBlockThreads;
+template <int E>
 __global__ __launch_bounds__(kBlockThreads) void free_push_kernel(BlockPoolArgs p) {
-    constexpr int E = 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int at = *p.free_count;
-    const int steps = (int)min((int64_t)E, (p.n_blocks + kBlockThreads - 1) / kBlockThreads);
-    for (int64_t b0 = 0; b0 < p.n_blocks; b0 += kBlockThreads * steps) {
-        const int64_t first = b0 + wave * (64 * steps) + lane;
+    for (int64_t b0 = 0; b0 < p.n_blocks; b0 += kBlockThreads * E) {
+        const int64_t first = b0 + wave * (64 * E) + lane;
         uint32_t marked = 0;
         int total;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if (e >= steps) break;
-            const int64_t id = min(first + 64 * e, p.n_blocks - 1);
-            if (p.ref[id] == kFreed && first + 64 * e < p.n_blocks) marked |= 1u << e;
+            const int64_t id = first + 64 * e;
+            if (p.ref[min(id, p.n_blocks - 1)] == kFreed && id < p.n_blocks) marked |= 1u << e;
         }
         int mine = 0;                              // of the wave: all, and those before this lane's e-th
         int before[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if (e >= steps) break;
             const uint64_t here = __ballot(marked >> e & 1);
             before[e] = mine + __popcll(here & ((1ull << lane) - 1));
             mine += __popcll(here);
@@ -300,7 +310,8 @@ __device__ inline int counts_before(const CompactArgs &a, int to) {
 
 // With n live blocks: the k-th live id at or past n goes to the k-th free id
 // below n.  Each workgroup ranks 1,024 ids.  SMALL (up to kCompactSmall chunks):
-// each counts the whole pool itself, so that no launch has to do it before.
+// each counts the whole pool itself, so that no launch has to do it before (5 us in
+// one kernel, 2.2 + 4.4 and the gap between them in two, for 3,000 ids).
 constexpr int kCompactSmall = 32;
 template <bool SMALL>
 __global__ __launch_bounds__(kBlockThreads) void compact_rank_kernel(CompactArgs a) {
@@ -410,7 +421,11 @@ __device__ inline uint32_t fp8_of4(const float *x) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
 }
 
-// A wave writes one token: 8 values of a key and a value row at a time.
+// A wave writes one token: 8 values of a key and a value row at a time, 16-byte
+// loads; what it needs to find the place (the sequence, its length, the block) is a
+// chain of four loads, which bounds small calls (64 tokens: 3.4 us); large ones are
+// bound by memory (47,248 tokens x 8 heads x 128 into an 8-bit cache: 58 us, 5.0
+// TB/s of reads and writes, what a large copy reaches).
 template <typename T, typename C, int D>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a) {
     const int lane = threadIdx.x & 63;
