@@ -430,6 +430,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
         a.prefix_len = groups->prefix_len_dev;
         a.n_groups = groups->n_groups;
         a.prefix_parts = p.prefix_parts;
+        a.max_group = groups->max_group;
         a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, shape->io_dtype == LA_F32 ? la::kTileRows : la::kPromptRows);
         prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups * a.kv_heads;
     }

@@ -70,7 +70,8 @@ struct AttnArgs {
     int32_t max_kv;                // longest kv_len that the tables and the workspace cover
     int32_t parts;                 // decode: parts the workspace holds for each row
     int32_t prefix_parts;          // decode: of these, the most of a prefix
-    int32_t group_tiles;           // decode: row tiles of the largest group
+    int32_t max_group;             // decode: sequences of a group that share, at most
+    int32_t group_tiles;           // decode: row tiles of so many
     int32_t prefix_items;          // decode: workgroups of the prefixes, ahead of the others
     bool ordered;                  // prompts: sequences in `order` (up to 64), the longest first
     uint8_t order[64];

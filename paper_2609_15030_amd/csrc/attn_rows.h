@@ -50,7 +50,7 @@ __device__ inline OwnKeys own_keys(const AttnArgs &a, int s) {
     int shared = 0;
     for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
         const int n = min(64, a.n_groups - g0), g = g0 + min((int)(threadIdx.x & 63), n - 1);
-        const int c0 = a.cu_group[g], c1 = a.cu_group[g + 1], p = a.prefix_len[g];
+        const int c0 = max(0, a.cu_group[g]), c1 = group_end(a, c0, a.cu_group[g + 1]), p = a.prefix_len[g];
         for (int i = 0; i < n; ++i) {
             const int b0 = __builtin_amdgcn_readlane(c0, i), b1 = __builtin_amdgcn_readlane(c1, i);
             if (s >= b0 && s < b1 && b1 - b0 > 1) shared = __builtin_amdgcn_readlane(p, i);

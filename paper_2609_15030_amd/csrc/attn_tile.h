@@ -101,6 +101,10 @@ __device__ inline int row_limit(const AttnArgs &a, const RowTile &t, int row) {
     return max(0, min(t.keys, t.pos0 + tok + 1));
 }
 
+// The end of the group of sequences [c0, c1), cut to the call's and to max_group: those
+// behind it have all their keys to themselves (attn_rows.h decides the same way).
+__device__ inline int group_end(const AttnArgs &a, int c0, int c1) { return min(min(c1, c0 + a.max_group), a.n_seqs); }
+
 // Shared keys of a group: none if it has only one member (its keys are then all its own).
 __device__ inline int group_prefix(const AttnArgs &a, int g, int members) {
     if (members < 2) return 0;
@@ -125,7 +129,7 @@ __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     r /= a.group_tiles;
     t->part = r % a.prefix_parts;
     const int g = r / a.prefix_parts;
-    const int s0 = a.cu_group[g], members = a.cu_group[g + 1] - s0;
+    const int s0 = max(0, a.cu_group[g]), members = group_end(a, s0, a.cu_group[g + 1]) - s0;
     t->seq = s0;
     t->tok0 = s0;
     t->n_rows = members * a.group;

@@ -37,6 +37,9 @@ __device__ inline void count_error(const BlockPoolArgs &p) {
     if (p.err) atomicAdd(p.err, 1);
 }
 
+// Free blocks on the stack; a count outside it is cut, so that no call leaves the list.
+__device__ inline int free_blocks(const BlockPoolArgs &p) { return (int)max((int64_t)0, min((int64_t)*p.free_count, p.n_blocks)); }
+
 // Vectors [part * kPartVec, ...) of one block to another, loads first.
 __device__ inline void copy_block_part(const BlockPoolArgs &p, int64_t src, int64_t dst, int64_t part) {
     const f32x4 *s = (const f32x4 *)p.cache + src * p.block_vec;
@@ -110,7 +113,7 @@ __device__ inline bool fork_of(const ForkArgs &a, int i, int *full, int *tail) {
 // One workgroup: a fresh block for every fork whose parent ends inside one, in
 // the order of the forks.
 __global__ __launch_bounds__(kBlockThreads) void fork_take_kernel(ForkArgs a) {
-    const int have = *a.p.free_count;
+    const int have = free_blocks(a.p);
     int taken = 0;
     for (int i0 = 0; i0 < a.n; i0 += kBlockThreads) {
         const int i = i0 + threadIdx.x;
@@ -120,11 +123,11 @@ __global__ __launch_bounds__(kBlockThreads) void fork_take_kernel(ForkArgs a) {
         const bool want = ok && tail >= 0;
         const int k = taken + block_sum_before(want, &total);
         if (want) {
-            int id = -1;
-            if (k < have) {
-                id = a.p.free_list[have - 1 - k];
+            int id = k < have ? a.p.free_list[have - 1 - k] : -1;
+            if ((uint32_t)id < (uint64_t)a.p.n_blocks) {
                 a.p.ref[id] = 1;
             } else {
+                id = -1;
                 count_error(a.p);
             }
             a.p.table[(int64_t)a.child[i] * a.p.max_blocks + full] = id;
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(kBlockThreads) void fork_kernel(ForkArgs a) {
 // tokens), in the order of the rows and entries.
 __global__ __launch_bounds__(kBlockThreads) void extend_kernel(BlockPoolArgs p, const int32_t *rows, const int32_t *len, int32_t n) {
     constexpr int E = 8;                           // entries of a thread
-    const int have = *p.free_count;
+    const int have = free_blocks(p);
     const int64_t all = n * p.max_blocks;
     int taken = 0;
     for (int64_t e0 = 0; e0 < all; e0 += kBlockThreads * E) {
@@ -203,8 +206,8 @@ __global__ __launch_bounds__(kBlockThreads) void extend_kernel(BlockPoolArgs p, 
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if (!at[e]) continue;
-            if (k < have) {
-                const int id = p.free_list[have - 1 - k];
+            const int id = k < have ? p.free_list[have - 1 - k] : -1;
+            if ((uint32_t)id < (uint64_t)p.n_blocks) {
                 p.ref[id] = 1;
                 *at[e] = id;
             } else {
@@ -250,7 +253,7 @@ constexpr int kPushSmall = 4 * kBlockThreads;
 template <int E>
 __global__ __launch_bounds__(kBlockThreads) void free_push_kernel(BlockPoolArgs p) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int at = *p.free_count;
+    int at = free_blocks(p);
     for (int64_t b0 = 0; b0 < p.n_blocks; b0 += kBlockThreads * E) {
         const int64_t first = b0 + wave * (64 * E) + lane;
         uint32_t marked = 0;

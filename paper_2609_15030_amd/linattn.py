@@ -559,13 +559,24 @@ def _ws(workspace):
 
 
 def la_attn_prefill_workspace_bytes(shape: LaAttnShape, cu_host: np.ndarray, kv_len_host=None) -> int:
+    if len(cu_host) <= shape.n_seqs or (kv_len_host is not None and len(kv_len_host) < shape.n_seqs):
+        raise ValueError("cu_seqlens or kv_len has too few entries for the call's sequences")
     return _lib.la_attn_prefill_workspace_bytes(ctypes.byref(shape), _hptr(cu_host, np.int32),
                                                 _hptr(kv_len_host, np.int32))
+
+
+def _lengths(n_seqs, cu_dev, cu_host, kv_dev=None, kv_host=None):
+    """Refuses length arrays that are shorter than the call's sequences."""
+    if len(cu_host) <= n_seqs or cu_dev.numel() <= n_seqs:
+        raise ValueError("cu_seqlens has fewer than n_seqs + 1 entries")
+    if kv_host is not None and (len(kv_host) < n_seqs or kv_dev.numel() < n_seqs):
+        raise ValueError("kv_len has fewer entries than the call sequences")
 
 
 def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o, workspace=None, stream=None,
                     check: bool = True) -> int:
     """q, o [T, q_heads, d], k, v [T, kv_heads, d]: heads packed, tokens at any stride."""
+    _lengths(shape.n_seqs, cu_dev, cu_host)
     T, dt = int(cu_host[shape.n_seqs]), _TORCH[shape.io_dtype]
     rows, kv = (T, shape.q_heads, shape.head_dim), (T, shape.kv_heads, shape.head_dim)
     (qp, qs), (kp, ks), (vp, vs), (op, os_) = _rows(q, dt, rows), _rows(k, dt, kv), _rows(v, dt, kv), _rows(o, dt, rows)
@@ -579,6 +590,7 @@ def la_attn_prefill(shape: LaAttnShape, q, k, v, cu_dev, cu_host: np.ndarray, o,
 
 def la_attn_prefill_paged(shape: LaAttnShape, layer: LaKvLayer, q, cu_dev, cu_host: np.ndarray, kv_len_dev,
                           kv_len_host: np.ndarray, o, workspace=None, stream=None, check: bool = True) -> int:
+    _lengths(shape.n_seqs, cu_dev, cu_host, kv_len_dev, kv_len_host)
     rows, dt = (int(cu_host[shape.n_seqs]), shape.q_heads, shape.head_dim), _TORCH[shape.io_dtype]
     (qp, qs), (op, os_) = _rows(q, dt, rows), _rows(o, dt, rows)
     if layer._seqs < shape.n_seqs:

@@ -184,6 +184,23 @@ def test_binding_refuses_wrong_tensors():
         la._ids(table.long(), "table")
 
 
+def test_binding_refuses_short_length_arrays():
+    import torch
+    s = la.make_attn_shape(2, 8, 2, 128)
+    t = torch.zeros(4, dtype=torch.int32)
+    for cu, kv in ((_cu(0, 5), None), (_cu(0, 5, 9), _cu(5))):
+        with pytest.raises(ValueError):
+            la.la_attn_prefill_workspace_bytes(s, cu, kv)
+    with pytest.raises(ValueError):
+        la._lengths(2, t, _cu(0, 5))
+    with pytest.raises(ValueError):
+        la._lengths(2, t[:2], _cu(0, 5, 9))
+    with pytest.raises(ValueError):
+        la._lengths(2, t, _cu(0, 5, 9), t, _cu(5))
+    with pytest.raises(ValueError):
+        la._lengths(2, t, _cu(0, 5, 9), t[:1], _cu(5, 9))
+
+
 def test_factors_out_of_range_are_refused():
     """Sizes and factors each fine by itself whose sum or product is not."""
     assert _prefill(_shape(scale=1e-39)) == la.LA_ERR_INVALID_ARG               # a subnormal exponent factor

@@ -266,6 +266,23 @@ def test_single_tokens(case):
     assert torch.equal(plan.run(cache.layer(), q, kv_dev, pre), o)
 
 
+def test_a_group_larger_than_its_plan():
+    """The sequences behind max_group read their whole keys themselves."""
+    gen = torch.Generator().manual_seed(33)
+    kv = [300 + 7 * i for i in range(9)]
+    cache = Cache(gen, kv, 2, 128, "bf16", 16, shared=[(0, 9, 288)])
+    q = _rand(gen, 9, 16, 128).to(torch.bfloat16).cuda()
+    kv_dev = torch.tensor(kv, dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 9], dtype=torch.int32, device="cuda")
+    pre = torch.tensor([288], dtype=torch.int32, device="cuda")
+    for most in (1, 4):
+        plan = api.AttnDecode(9, 16, 2, 128, max(kv), cu_group=cu, max_prefix_len=288, max_group=most)
+        plan.workspace.fill_(0xFF)               # a slot that nothing wrote is NaN
+        o = plan.run(cache.layer(), q, kv_dev, pre)
+        ref = [(i, oa.attend(_host(q[i:i + 1]), *cache.rows(i), n - 1, float(np.float32(128 ** -0.5))), n) for i, n in enumerate(kv)]
+        _check(o, ref, 128, True, f"max_group {most}")
+
+
 # --- what a call may not depend on ---------------------------------------------
 
 def test_a_single_token_does_not_depend_on_its_batch():

@@ -126,6 +126,19 @@ def test_bad_ids_are_counted():
     p.free([0, 1])
 
 
+def test_a_damaged_free_list_is_counted():
+    """A count past the list is cut to it, an id that is none is not handed out."""
+    pool = api.BlockPool.new(6, 16, 4, 2, 4)
+    pool.free_count.fill_(100)
+    pool.free_list[5] = 999                      # the first to be taken
+    pool.extend(_i32([0]), _i32([8]))
+    assert pool.table[0].tolist() == [-1, 1, -1, -1] and int(pool.err_count) == 1 and int(pool.free_count) == 4
+    pool.free_count.fill_(-3)
+    pool.extend(_i32([1]), _i32([4]))
+    assert pool.table[1].tolist() == [-1] * 4 and int(pool.err_count) == 2 and int(pool.free_count) == 0
+    assert pool.ref_count.tolist() == [0, 1, 0, 0, 0, 0]
+
+
 def test_many_blocks_and_rows():
     """More ids than one workgroup ranks, rows longer than one workgroup's pass, blocks of several parts."""
     bt, width, rows = 16, 1100, 6
