@@ -464,7 +464,9 @@ _I32 = torch.int32
 def _rows(t, dtype, shape):
     """(device pointer, elements from one token to the next) of a [tokens, heads,
     dim] tensor whose heads are packed within a token (a slice of a wider
-    projection will do); 0 stands for packed tokens."""
+    projection will do); 0 stands for packed tokens.  Tokens that overlap (a
+    tensor expanded over them has stride 0) are refused: the library would walk
+    past the memory that they have."""
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise ValueError(f"expected a {dtype} device tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if t.is_contiguous():
@@ -472,7 +474,11 @@ def _rows(t, dtype, shape):
     n, heads, dim = shape
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
         raise ValueError("expected packed heads within a token")
-    return t.data_ptr(), t.stride(0) if n > 1 else 0
+    if n <= 1:
+        return t.data_ptr(), 0
+    if t.stride(0) < heads * dim:
+        raise ValueError(f"expected tokens at least {heads * dim} elements apart, got a stride of {t.stride(0)}")
+    return t.data_ptr(), t.stride(0)
 
 
 def _dtype_of(dtype) -> int:
