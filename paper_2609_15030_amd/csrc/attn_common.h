@@ -177,7 +177,7 @@ struct Runs {
         if (!ok && s.err) atomicAdd(s.err, 1);
         const int t = base + kRunTokens * (int)(threadIdx.x & 63);
         at = (int64_t)(ok ? id : 0) * s.block_bytes +
-             (int64_t)(((kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1))) * row_bytes);
+             (int64_t)((kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1))) * row_bytes;    // may pass 2 GB within a block
     }
     __device__ inline int64_t run(int r) const {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r);
