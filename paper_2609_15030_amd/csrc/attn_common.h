@@ -167,17 +167,19 @@ constexpr int kRunTokens = 16;
 struct Runs {
     int64_t at;
     uint64_t bad;
-    __device__ static inline int fetch(const KvSource &s, const int32_t *table_row, int base, int hi) {
-        const int t = base + kRunTokens * (int)(threadIdx.x & 63);
-        return t < hi ? table_row[t >> s.bt_shift] : 0;
+    // The lane's block id of the 1,024 tokens `ahead` of base.  Compared by distance: a
+    // sequence may end so near 2^31 that the token itself passes it.
+    __device__ static inline int fetch(const KvSource &s, const int32_t *table_row, int base, int ahead, int hi) {
+        const int off = ahead + kRunTokens * (int)(threadIdx.x & 63);
+        return off < hi - base ? table_row[(base + off) >> s.bt_shift] : 0;
     }
     __device__ inline void set(const KvSource &s, int id, int base, int kvh, int row_bytes) {
         const bool ok = (uint32_t)id < (uint32_t)s.n_blocks;
         bad = __ballot(!ok);
         if (!ok && s.err) atomicAdd(s.err, 1);
-        const int t = base + kRunTokens * (int)(threadIdx.x & 63);
+        const uint32_t t = (uint32_t)base + kRunTokens * (threadIdx.x & 63);
         at = (int64_t)(ok ? id : 0) * s.block_bytes +
-             (int64_t)((kvh << s.bt_shift) + (t & ((1 << s.bt_shift) - 1))) * row_bytes;    // may pass 2 GB within a block
+             (int64_t)((kvh << s.bt_shift) + (int)(t & ((1u << s.bt_shift) - 1))) * row_bytes;    // may pass 2 GB within a block
     }
     __device__ inline int64_t run(int r) const {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r);

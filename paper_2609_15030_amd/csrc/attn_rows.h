@@ -129,7 +129,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         // the part's runs of 16 keys, one a lane
         static_assert(kOwnPart <= 64 * kRunTokens, "a lane for each run");
         Runs runs;
-        runs.set(a.kv, Runs::fetch(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo, hi), lo, kvh, RB);
+        runs.set(a.kv, Runs::fetch(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo, 0, hi), lo, kvh, RB);
         uint4 qf[NQ];
         {
             const T *qp = (const T *)a.q + seq * a.q_stride + (int64_t)head * D;
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(256) void attn_join_prompt_kernel(AttnArgs a) {
     const int lane = threadIdx.x % LANES, row = local * ROWS + threadIdx.x / LANES;
     if (row >= new_tokens * heads) return;
     const int tok = a.by_group(a.by_kv_heads(row)), head = row - tok * heads;
-    const int limit = max(0, keys - new_tokens + tok + 1), parts = (limit + (1 << a.part_shift) - 1) >> a.part_shift;
+    const int limit = max(0, keys - new_tokens + tok + 1), parts = (int)(((uint32_t)limit + (1u << a.part_shift) - 1) >> a.part_shift);
     const int64_t slot = slots + (int64_t)row * stride;
     const float2 *ml = a.part_ml + slot;
     const float *po = a.part_o + slot * D + 4 * lane;

@@ -32,8 +32,8 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
     __device__ inline void begin(const KvSource &s, int lo) {
         if constexpr (PAGED) {
             base = lo & ~(64 * kRunTokens - 1);
-            const int id = Runs::fetch(s, table_row, base, hi);
-            next = Runs::fetch(s, table_row, base + 64 * kRunTokens, hi);
+            const int id = Runs::fetch(s, table_row, base, 0, hi);
+            next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
             runs.set(s, id, base, kvh, RB);
         }
     }
@@ -43,7 +43,7 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
             if (t0 - base >= 64 * kRunTokens) {
                 base += 64 * kRunTokens;
                 runs.set(s, next, base, kvh, RB);
-                next = Runs::fetch(s, table_row, base + 64 * kRunTokens, hi);
+                next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
             }
             const int r0 = ((t0 - base) + wave * RPL) / kRunTokens;
             p->missing = 0;
@@ -196,7 +196,7 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
         t->lo = 0;
         if (t->n_parts > 1) {
             t->lo = t->part << a.part_shift;
-            t->hi = min(t->hi, t->lo + (1 << a.part_shift));
+            t->hi = t->lo + min(t->hi - t->lo, 1 << a.part_shift);      // lo + 2^part_shift may be 2^31
             return t->lo < t->hi;
         }
         return true;

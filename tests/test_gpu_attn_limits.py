@@ -46,3 +46,39 @@ def test_a_layer_whose_keys_take_over_2_gb_of_a_block(kind, heads):
     x = [y[:, some] for y in (q, k, v)]
     _check(got[:, some], *x, 0, d, kind == "bf16", f"{heads} heads, prompt")
     _check(one[:, some], x[0][n - 1:], *x[1:], n - 1, d, kind == "bf16", f"{heads} heads, single token")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_the_longest_sequence(kind):
+    """2^31 - 256 keys, all but the last block's in one block (the table names it
+    again and again): zero keys, so equal weights, and the same values in every
+    token.  The last block's keys score +-64 against them: the first query head
+    sees that block alone (e^-64 of 2^31 others is 3e-19), the second the others,
+    whose sums of small whole numbers are exact in fp32."""
+    d, bt, last, t = 64, 256, 0x7FFFFF00, TYPES[kind]
+    part = bt * d * torch.empty(0, dtype=t).element_size()
+    cache = torch.zeros((2, 2 * part), dtype=torch.uint8, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(62)
+    k = 0.02 * torch.randn((bt, 1, d), generator=gen, device="cuda")
+    k[..., 0] = 16.0
+    v = torch.randn((bt, 1, d), generator=gen, device="cuda")
+    k, v = k.to(t), v.to(t)
+    whole = (torch.arange(d, device="cuda") % 4 + 1).to(t)
+    keys, values = (cache[:, i * part:(i + 1) * part].view(t).unflatten(1, (bt, d)) for i in (0, 1))
+    keys[1], values[1], values[0] = k[:, 0], v[:, 0], whole
+    table = torch.zeros((1, last // bt), dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    layer = la.make_kv_layer(cache, table, bt, 1, d, t, err_count=err)
+    q = torch.zeros((1, 2, d), device="cuda")
+    q[0, :, 0] = torch.tensor([32.0, -32.0], device="cuda")           # scores: +-32 x 16 / 8
+    q = q.to(t)
+    kv = torch.tensor([last], dtype=torch.int32, device="cuda")
+    for what, o in (("prompt", api.AttnPrefill(2, 1, d, [1], [last], dtype=t).run_paged(layer, q)),
+                    ("single token", api.AttnDecode(1, 2, 1, d, last, dtype=t).run(layer, q, kv))):
+        torch.cuda.synchronize()
+        assert int(err) == 0
+        _check(o[:, :1], q[:, :1], k, v, bt - 1, d, kind == "bf16", f"longest sequence, {what}")
+        # a quotient of exact sums by way of a reciprocal: three roundings of the fp32, one of the type
+        off = (o[0, 1].double() - whole.double()).abs() / whole.double()
+        assert float(off.max()) <= (2 ** -8 if kind == "bf16" else 4 * 2 ** -24), (what, float(off.max()))
