@@ -85,7 +85,7 @@ la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
         return fail(LA_ERR_INVALID_ARG, "k_scale=%g and v_scale=%g must be positive and finite", (double)y->k_scale, (double)y->v_scale);
     if (y->dtype != LA_FP8_E4M3 && (y->k_scale != 1.f || y->v_scale != 1.f))
         return fail(LA_ERR_INVALID_ARG, "scales other than 1 go with an 8-bit cache");
-    if (y->max_blocks < 1 || y->max_blocks * bt > 0x7fffff00)
+    if (y->max_blocks < 1 || y->max_blocks > 0x7fffff00 / bt)
         return fail(LA_ERR_INVALID_ARG, "max_blocks=%lld must be positive and cover fewer than 2^31 tokens", (long long)y->max_blocks);
     if (!y->block_table) return fail(LA_ERR_INVALID_ARG, "block_table is required");
     if (!y->cache || !aligned16(y->cache))
