@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kBlockThreads) void fork_kernel(ForkArgs a) {
     const int32_t *src = p.table + (int64_t)a.parent[i] * p.max_blocks;
     int32_t *dst = p.table + (int64_t)a.child[i] * p.max_blocks;
     if (blockIdx.x == 0) {
-        for (int j = threadIdx.x; j < p.max_blocks; j += kBlockThreads) {
+        for (int64_t j = threadIdx.x; j < p.max_blocks; j += kBlockThreads) {      // 64 bits: a row may have 2^31 - 1 entries
             if (j == full && tail >= 0) continue;
             int id = j < full ? src[j] : -1;
             if (id != -1 && (uint32_t)id >= (uint64_t)p.n_blocks) {
