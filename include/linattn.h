@@ -581,7 +581,9 @@ la_status la_blocks_copy(const la_block_pool *pool, const int32_t *src_ids_dev, 
  * last block inside which the tokens end is copied into a fresh one, so that
  * parent and child can both go on.  What the child's row held before is
  * overwritten.  Children are distinct and no parents of the same call; at
- * most 65,535 forks.  A fork that finds no free block gets -1 there. */
+ * most 65,535 forks.  A fork that finds no free block, or whose parent has no
+ * block where its tokens end, gets -1 there and counts; where the parent has no
+ * block among the whole ones, the child has none either. */
 la_status la_blocks_fork(const la_block_pool *pool, const int32_t *parent_rows_dev, const int32_t *child_rows_dev,
                          const int32_t *len_dev, int64_t n, void *stream);
 

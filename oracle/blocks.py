@@ -57,7 +57,9 @@ class Book:
                     self.ref[b] += 1
                 else:
                     self.errors += 1
-            if n % self.bt and self._ok(self.table[p, full]):
+            if n % self.bt and not self._ok(self.table[p, full]):
+                self.errors += 1                         # nothing to copy
+            elif n % self.bt:
                 row[full] = self._take()
                 if row[full] >= 0:
                     self.cache[row[full]] = self.cache[self.table[p, full]]

@@ -95,7 +95,8 @@ struct ForkArgs {
 };
 
 // What fork i does: false if its rows are no rows.  *full: whole blocks shared;
-// *tail: the parent's last block, inside which its tokens end (-1: none).
+// *tail: the parent's last block, inside which its tokens end (-1: they end with a
+// whole block; -2: the parent has no block there).
 __device__ inline bool fork_of(const ForkArgs &a, int i, int *full, int *tail) {
     const int pr = a.parent[i], ch = a.child[i];
     if (pr < 0 || pr >= a.p.n_rows || ch < 0 || ch >= a.p.n_rows || pr == ch) return false;
@@ -105,7 +106,7 @@ __device__ inline bool fork_of(const ForkArgs &a, int i, int *full, int *tail) {
     *tail = -1;
     if (len & ((1 << a.p.bt_shift) - 1)) {
         const int id = a.p.table[(int64_t)pr * a.p.max_blocks + *full];
-        if ((uint32_t)id < (uint64_t)a.p.n_blocks) *tail = id;
+        *tail = (uint32_t)id < (uint64_t)a.p.n_blocks ? id : -2;
     }
     return true;
 }
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kBlockThreads) void fork_take_kernel(ForkArgs a) {
         const int i = i0 + threadIdx.x;
         int full = 0, tail = -1, total;
         const bool ok = i < a.n && fork_of(a, i, &full, &tail);
-        if (i < a.n && (!ok || a.len[i] < 0 || a.len[i] > (a.p.max_blocks << a.p.bt_shift))) count_error(a.p);
+        if (i < a.n && (!ok || tail == -2 || a.len[i] < 0 || a.len[i] > (a.p.max_blocks << a.p.bt_shift))) count_error(a.p);
         const bool want = ok && tail >= 0;
         const int k = taken + block_sum_before(want, &total);
         if (want) {
