@@ -598,7 +598,8 @@ la_status la_blocks_free(const la_block_pool *pool, const int32_t *rows_dev, int
 
 /* la_blocks_compact - moves the L live blocks into ids 0 .. L-1: the k-th live
  * id at or past L goes to the k-th free id below L.  Table, counts and free
- * list follow (the lowest free id on top).  new_ids_dev ([n_blocks], may be
+ * list follow (the lowest free id on top); an entry that names a free block
+ * becomes -1 and counts.  new_ids_dev ([n_blocks], may be
  * NULL) receives every block's new id, -1 for free ones, for tables kept
  * elsewhere. */
 la_status la_blocks_compact(const la_block_pool *pool, int32_t *new_ids_dev, void *workspace, size_t ws_bytes,

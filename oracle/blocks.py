@@ -110,7 +110,13 @@ class Book:
         self.ref[n:] = 0
         for r in range(self.table.shape[0]):
             for j in range(self.table.shape[1]):
-                if self.table[r, j] >= 0:
-                    self.table[r, j] = new[self.table[r, j]]
+                b = self.table[r, j]
+                if b == -1:
+                    continue
+                if not self._ok(b):
+                    self.errors += 1
+                    continue
+                self.errors += int(new[b] < 0)           # it named a free block
+                self.table[r, j] = new[b]
         self.free = list(range(len(self.ref) - 1, n - 1, -1))
         return new

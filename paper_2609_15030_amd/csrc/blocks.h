@@ -379,13 +379,18 @@ __global__ __launch_bounds__(kBlockThreads) void compact_move_kernel(CompactArgs
         const int64_t e = (int64_t)b * kBlockThreads + threadIdx.x;
         if (e >= p.n_rows * p.max_blocks) return;
         const int id = p.table[e];
-        if (id < n || id >= p.n_blocks) {
-            if (id >= p.n_blocks || id < -1) count_error(p);
+        if (id == -1) return;
+        if ((uint32_t)id >= (uint64_t)p.n_blocks) {
+            count_error(p);
             return;
         }
         const int k = a.rank[id];
-        if (k >= 0) p.table[e] = a.dst[k];
-        else count_error(p);                       // an entry that names a free block
+        if (k < 0) {                               // a free block: left there, the entry would name what moves in
+            p.table[e] = -1;
+            count_error(p);
+        } else if (id >= n) {
+            p.table[e] = a.dst[k];
+        }
         return;
     }
     b -= table_blocks;
