@@ -517,7 +517,7 @@ size_t la_attn_prefill_workspace_bytes(const la_attn_shape *shape, const int32_t
  * first sequence.  Any length serves, whole blocks or not. */
 typedef struct la_prefix_groups {
     int32_t n_groups;
-    int32_t max_group;               /* sequences of the largest group; those past it in a larger one share nothing */
+    int32_t max_group;               /* sequences of the largest group (0: all are empty); those past it in a larger one share nothing */
     const int32_t *cu_group_dev;     /* device [n_groups + 1]                       */
     const int32_t *prefix_len_dev;   /* device [n_groups]                           */
     int64_t max_prefix_len;          /* at least every prefix_len                   */

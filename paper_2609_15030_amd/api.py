@@ -188,7 +188,8 @@ class AttnDecode:
 
     cu_group: device int32 [n_groups + 1], the groups of consecutive sequences
     that share a prefix of at most max_prefix_len keys (None: nothing shared);
-    max_group: the most sequences of a group (None: read from cu_group)."""
+    max_group: the most sequences of a group (None: read from cu_group; n_seqs
+    where its groups are all empty, since they may be filled later)."""
 
     def __init__(self, n_seqs: int, q_heads: int, kv_heads: int, head_dim: int, max_kv_len: int,
                  dtype=torch.bfloat16, scale: Optional[float] = None, cu_group: Optional[torch.Tensor] = None,
@@ -196,7 +197,7 @@ class AttnDecode:
         self.shape = la.make_attn_shape(n_seqs, q_heads, kv_heads, head_dim, la._dtype_of(dtype), scale)
         self.max_kv_len, self.cu_group, self.max_prefix_len = int(max_kv_len), cu_group, int(max_prefix_len)
         if cu_group is not None and max_group is None:
-            max_group = int((cu_group[1:] - cu_group[:-1]).max()) if cu_group.numel() > 1 else 0
+            max_group = (int((cu_group[1:] - cu_group[:-1]).max()) if cu_group.numel() > 1 else 0) or n_seqs
         self.max_group = max_group
         self.o = torch.empty((n_seqs, q_heads, head_dim), dtype=dtype, device=device)
         n = la.la_attn_decode_workspace_bytes(self.shape, self.max_kv_len, self.max_prefix_len)

@@ -402,7 +402,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     if (groups && groups->n_groups < 0) return fail(LA_ERR_INVALID_ARG, "n_groups=%d", groups->n_groups);
     if (shared && (!groups->cu_group_dev || !groups->prefix_len_dev))
         return fail(LA_ERR_INVALID_ARG, "cu_group_dev and prefix_len_dev are required with a shared prefix");
-    if (shared && (groups->max_group < 1 || groups->max_group > shape->n_seqs))
+    if (shared && (groups->max_group < 0 || groups->max_group > shape->n_seqs))
         return fail(LA_ERR_INVALID_ARG, "max_group=%d of %d sequences", groups->max_group, shape->n_seqs);
     const DecodePlan p = plan_decode(max_kv_len, max_prefix);
     a.parts = p.own_parts + p.prefix_parts;
