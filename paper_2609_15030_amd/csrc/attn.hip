@@ -21,7 +21,9 @@ using la::host::aligned16;
 using la::host::fail;
 using la::host::hip_check;
 
-constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxInt = 0x7fffffff;
+// A launch has fewer than 2^32 threads along an axis: workgroups of `threads`, at most.
+constexpr int64_t max_grid(int threads) { return 0xffffffffll / threads; }
 
 int64_t dtype_size(int32_t d) { return d == LA_F32 ? 4 : d == LA_BF16 ? 2 : 1; }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -175,7 +177,8 @@ la_status plan_prompt(const la_attn_shape *s, const int32_t *cu, const int32_t *
             p->slots += rows * parts;
             p->joins += up(rows, 1024 / s->head_dim);
         }
-    if (p->items * s->kv_heads > kMaxGrid || p->slots > kMaxGrid)
+    static_assert(la::kWideThreads == 256 && la::kTileThreads == 256, "workgroups of a prompt");
+    if (p->items * s->kv_heads > max_grid(256) || p->joins > max_grid(256) || p->slots > kMaxInt)
         return fail(LA_ERR_INVALID_ARG, "too many row tiles for one launch");
     return LA_OK;
 }
@@ -318,10 +321,15 @@ la_status check_rows(const void *rows, int64_t n, const char *what) {
 }
 
 template <typename T, typename C>
-void launch_kv_write(int d, const la::KvWriteArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)up(a.n_tokens, la::kWriteTokens));
-    if (d == 64) hipLaunchKernelGGL((la::kv_write_kernel<T, C, 64>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((la::kv_write_kernel<T, C, 128>), grid, dim3(256), 0, st, a);
+la_status launch_kv_write(int d, la::KvWriteArgs &a, hipStream_t st) {
+    constexpr int64_t STEP = max_grid(256) * la::kWriteTokens;
+    for (a.first_token = 0; a.first_token < a.n_tokens; a.first_token += STEP) {
+        const dim3 grid((unsigned)up(std::min(a.n_tokens - a.first_token, STEP), la::kWriteTokens));
+        if (d == 64) hipLaunchKernelGGL((la::kv_write_kernel<T, C, 64>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((la::kv_write_kernel<T, C, 128>), grid, dim3(256), 0, st, a);
+        if (la_status e = hip_check("cache write launch")) return e;
+    }
+    return LA_OK;
 }
 
 }  // namespace
@@ -434,7 +442,7 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
         a.group_tiles = (int32_t)up((int64_t)groups->max_group * a.group, shape->io_dtype == LA_F32 ? la::kTileRows : la::kPromptRows);
         prefix_items = (int64_t)a.group_tiles * p.prefix_parts * groups->n_groups * a.kv_heads;
     }
-    if (items > kMaxGrid || rows > kMaxGrid || prefix_items + kRowsGrid > kMaxGrid)
+    if (items > kMaxInt || rows > max_grid(256) || prefix_items + kRowsGrid > max_grid(la::kRowsThreads))
         return fail(LA_ERR_INVALID_ARG, "too many parts for one launch");
     a.prefix_items = (int32_t)prefix_items;
     const int64_t blocks = std::min<int64_t>(items, kRowsGrid);
@@ -479,22 +487,26 @@ la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k,
     a.n_blocks = (int32_t)layer->n_blocks;
     a.bt_shift = shift_of(layer->block_tokens);
     (void)hipGetLastError();
-    if (layer->dtype == LA_F32) launch_kv_write<float, float>(layer->head_dim, a, (hipStream_t)stream);
-    else if (layer->dtype == LA_BF16) launch_kv_write<__bf16, __bf16>(layer->head_dim, a, (hipStream_t)stream);
-    else launch_kv_write<__bf16, la::fp8_t>(layer->head_dim, a, (hipStream_t)stream);
-    return hip_check("cache write launch");
+    if (layer->dtype == LA_F32) return launch_kv_write<float, float>(layer->head_dim, a, (hipStream_t)stream);
+    if (layer->dtype == LA_BF16) return launch_kv_write<__bf16, __bf16>(layer->head_dim, a, (hipStream_t)stream);
+    return launch_kv_write<__bf16, la::fp8_t>(layer->head_dim, a, (hipStream_t)stream);
 }
 
 la_status la_blocks_copy(const la_block_pool *pool, const int32_t *src_ids_dev, const int32_t *dst_ids_dev, int64_t n, void *stream) {
     la::BlockPoolArgs p{};
     if (la_status e = check_pool(pool, false, true, &p)) return e;
-    if (n < 0 || n > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "n=%lld", (long long)n);
+    if (n < 0 || n > kMaxInt) return fail(LA_ERR_INVALID_ARG, "n=%lld", (long long)n);
     if (n == 0) return LA_OK;
     if (!src_ids_dev || !dst_ids_dev) return fail(LA_ERR_INVALID_ARG, "src_ids and dst_ids are required");
     (void)hipGetLastError();
-    hipLaunchKernelGGL(la::blocks_copy_kernel, dim3((unsigned)n, (unsigned)up(p.block_vec, la::kPartVec)), dim3(la::kBlockThreads), 0,
-                       (hipStream_t)stream, p, src_ids_dev, dst_ids_dev);
-    return hip_check("block copy launch");
+    constexpr int64_t STEP = max_grid(la::kBlockThreads);
+    for (int64_t i = 0; i < n; i += STEP) {
+        const dim3 grid((unsigned)std::min(n - i, STEP), (unsigned)up(p.block_vec, la::kPartVec));
+        hipLaunchKernelGGL(la::blocks_copy_kernel, grid, dim3(la::kBlockThreads), 0, (hipStream_t)stream, p, src_ids_dev + i,
+                           dst_ids_dev + i);
+        if (la_status e = hip_check("block copy launch")) return e;
+    }
+    return LA_OK;
 }
 
 la_status la_blocks_fork(const la_block_pool *pool, const int32_t *parent_rows_dev, const int32_t *child_rows_dev,
@@ -562,7 +574,7 @@ la_status la_blocks_compact(const la_block_pool *pool, int32_t *new_ids_dev, voi
     a.remap = new_ids_dev;
     const int64_t parts = up(a.p.block_vec, la::kPartVec), table_blocks = up(a.p.n_rows * a.p.max_blocks, la::kBlockThreads);
     const int64_t copy_blocks = std::min<int64_t>(a.p.n_blocks * parts, 2048);
-    if (copy_blocks + table_blocks + a.n_chunks > kMaxGrid) return fail(LA_ERR_INVALID_ARG, "the table is too large for one launch");
+    if (copy_blocks + table_blocks + a.n_chunks > max_grid(la::kBlockThreads)) return fail(LA_ERR_INVALID_ARG, "the table is too large for one launch");
     hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
     if (a.n_chunks <= la::kCompactSmall) {

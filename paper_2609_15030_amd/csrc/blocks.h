@@ -412,7 +412,7 @@ struct KvWriteArgs {
     const void *k, *v;
     int64_t k_stride, v_stride;    // elements from one token to the next
     char *ck, *cv;                 // the layer's keys and values in block 0
-    int64_t block_bytes, max_blocks, n_tokens;
+    int64_t block_bytes, max_blocks, n_tokens, first_token;    // first_token: the launch's
     const int32_t *table, *cu, *kv_len;
     int32_t *err;
     float k_scale, v_scale;        // what a stored 8-bit 1 stands for
@@ -438,7 +438,7 @@ __device__ inline uint32_t fp8_of4(const float *x) {
 template <typename T, typename C, int D>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a) {
     const int lane = threadIdx.x & 63;
-    const int64_t tok = (int64_t)blockIdx.x * kWriteTokens + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t tok = a.first_token + (int64_t)blockIdx.x * kWriteTokens + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (tok >= a.n_tokens) return;
     int seq, local;
     if (!item_of(a.n_seqs, (int)tok, [&](int i) { return a.cu[i + 1] - a.cu[i]; }, &seq, &local)) return;

@@ -82,3 +82,21 @@ def test_the_longest_sequence(kind):
         # a quotient of exact sums by way of a reciprocal: three roundings of the fp32, one of the type
         off = (o[0, 1].double() - whole.double()).abs() / whole.double()
         assert float(off.max()) <= (2 ** -8 if kind == "bf16" else 4 * 2 ** -24), (what, float(off.max()))
+
+
+def test_writes_of_more_tokens_than_a_launch_has_waves():
+    """2^32 threads are 67,108,864 tokens of a wave each."""
+    bt, d, n = 256, 64, (1 << 26) + 1000
+    blocks = -(-n // bt)
+    k = torch.randint(-32768, 32768, (n, 1, d), dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    cache = torch.zeros((blocks, 2 * bt * d * 2), dtype=torch.uint8, device="cuda")
+    table = torch.arange(blocks, dtype=torch.int32, device="cuda")[None]
+    layer = la.make_kv_layer(cache, table, bt, 1, d, torch.bfloat16)
+    cu, kv = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, n], [n]))
+    la.la_kv_write(layer, k, k, cu, kv)
+    torch.cuda.synchronize()
+    halves = cache.view(torch.int16).view(blocks, 2, bt, d)
+    for half in (0, 1):
+        for a in range(0, blocks, 1 << 16):
+            got, want = halves[a:a + (1 << 16), half].reshape(-1, d), k[a * bt:(a + (1 << 16)) * bt, 0].view(torch.int16)
+            assert torch.equal(got[:len(want)], want) and not bool(got[len(want):].any())

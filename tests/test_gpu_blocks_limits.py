@@ -25,3 +25,15 @@ def test_a_fork_of_the_longest_row():
     assert torch.equal(table[0], table[1])
     assert [int(table[0, j]) for j in (0, 1, 1 << 30, width - 1)] == [2, -1, 0, 3]
     assert pool.ref_count.tolist() == [2, 0, 2, 2] and int(pool.err_count) == 0 and int(pool.free_count) == 4
+
+
+def test_copies_of_more_blocks_than_a_launch_has_workgroups():
+    """2^32 threads are 4,194,304 workgroups of 1,024."""
+    n = (1 << 22) + 50
+    pool = api.BlockPool.new(2 * n, 16, 16, 1, 1)
+    pool.cache[:n] = torch.randint(0, 256, (n, 16), dtype=torch.uint8, device="cuda")
+    pool.cache[n:] = 7
+    order = torch.randperm(n, device="cuda").to(torch.int32)
+    pool.copy(torch.arange(n, dtype=torch.int32, device="cuda"), n + order)
+    torch.cuda.synchronize()
+    assert torch.equal(pool.cache[n:][order.long()], pool.cache[:n]) and int(pool.err_count) == 0
