@@ -441,7 +441,8 @@ la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const i
  * sees no key (or whose every score is -inf) has o = 0; keys and values that
  * it does not see have no effect on it, infinities and NaN included (one
  * exception: an infinite value with a weight that rounds to zero gives
- * infinity or NaN).  Scores, maxima and sums are fp32; with bf16 inputs the
+ * infinity or NaN).  Scores, maxima and sums are fp32 (a token with a score past
+ * fp32's range has NaN); with bf16 inputs the
  * weights p_j are rounded to bf16 for the product with v.  The same call
  * gives the same bits.  A single token's result does not depend on the other
  * sequences of its call (its group's prefix apart); a prompt's keys are summed

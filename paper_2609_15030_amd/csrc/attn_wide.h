@@ -134,7 +134,8 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
         float shrink = 1.f;
         if (top > m + kLag) {
             shrink = __builtin_amdgcn_exp2f(m - top);
-            m = mu = top;
+            m = top;
+            mu = top + (top - top);              // a score past fp32's range: NaN, where infinity would weigh every key 0
         }
         l *= shrink;
         float e[16];

@@ -100,3 +100,50 @@ def test_writes_of_more_tokens_than_a_launch_has_waves():
         for a in range(0, blocks, 1 << 16):
             got, want = halves[a:a + (1 << 16), half].reshape(-1, d), k[a * bt:(a + (1 << 16)) * bt, 0].view(torch.int16)
             assert torch.equal(got[:len(want)], want) and not bool(got[len(want):].any())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_scores_past_the_range_of_fp32(kind):
+    """<q, k> = +-2^120 is finite, times a scale of 2^10 it is not: tokens that see such
+    a score have NaN (not 0, which stands for no key), those before it are as they
+    were, and one of minus infinity weighs nothing.  Prompts, single tokens and a
+    shared prefix alike."""
+    d, n, t = 64, 150, TYPES[kind]
+    gen = torch.Generator(device="cuda").manual_seed(63)
+    q, k, v = (torch.randn((n, h, d), generator=gen, device="cuda") for h in (2, 1, 1))
+    q, k = q * 2.0 ** -10, k.clone()
+    q[..., 0] = 0
+    k[..., 0] = 0
+    q, k, v = q.to(t), k.to(t), v.to(t)
+    plan = api.AttnPrefill(2, 1, d, [n], dtype=t, scale=2.0 ** 10)
+    clean = plan.run(q, k, v).clone()
+    q2, k2 = q.clone(), k.clone()
+    q2[:, 0, 0], q2[:, 1, 0] = 2.0 ** 60, -2.0 ** 60
+    k2[100, 0, 0] = 2.0 ** 60
+    o = plan.run(q2, k2, v)
+    torch.cuda.synchronize()
+    assert torch.equal(o[:100], clean[:100])
+    assert torch.isnan(o[100:, 0]).all() and torch.isfinite(o[100:, 1]).all()
+    # the second head: as without that key
+    _check_without(o[149:, 1:], q[149:, 1:], k, v, 100, 2.0 ** 10, kind == "bf16")
+    bt = 16
+    table = torch.arange(-(-n // bt), dtype=torch.int32, device="cuda").expand(3, -1).contiguous()
+    cache = torch.zeros((table.shape[1], 2 * bt * d * q.element_size()), dtype=torch.uint8, device="cuda")
+    layer = la.make_kv_layer(cache, table, bt, 1, d, t)
+    kv = torch.full((3,), n, dtype=torch.int32, device="cuda")
+    la.la_kv_write(layer, k2, v, torch.tensor([0, n], dtype=torch.int32, device="cuda"), kv)
+    cu, shared = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 3], [144]))
+    rows = q2[147:].contiguous()
+    for groups in (None, cu):
+        dec = api.AttnDecode(3, 2, 1, d, n, t, 2.0 ** 10, groups, 0 if groups is None else 144)
+        one = dec.run(layer, rows, kv, None if groups is None else shared)
+        torch.cuda.synchronize()
+        assert torch.isnan(one[:, 0]).all() and torch.isfinite(one[:, 1]).all()
+        _check_without(one[2:, 1:], q[149:, 1:], k, v, 100, 2.0 ** 10, kind == "bf16")
+
+
+def _check_without(o, q, k, v, key, scale, bf16):
+    """One token's o against attention over all keys but `key`."""
+    rest = [j for j in range(k.shape[0]) if j != key]
+    ref, mean, size = oa.attend(_host(q), _host(k)[rest], _host(v)[rest], len(rest) - 1, scale)
+    assert np.all(np.abs(_host(o) - ref) <= oa.tolerance(ref, mean, size, len(rest), q.shape[2], bf16))
