@@ -44,3 +44,55 @@ def test_groups_that_are_empty_at_first(io, kind):
     plan.workspace.fill_(0xFF)
     la.la_attn_decode(plan.shape, cache.layer(), q, kv_dev, 301, plan.o, none, plan.workspace)
     _check(plan.o, _ref(q, cache, d), d, io == "bf16", f"max_group 0, {kind}")
+
+
+@pytest.mark.parametrize("io,kind,d", [("bf16", "bf16", 128), ("bf16", "fp8", 64), ("f32", "f32", 128)])
+@pytest.mark.parametrize("prefix", [0, 40, 256])
+def test_own_keys_around_the_end_of_a_part(io, kind, d, prefix):
+    """Own keys of 255 to 257 and 511 to 513 tokens, from their 16-token line on: whole, and behind a prefix."""
+    gen = torch.Generator().manual_seed(72)
+    line = prefix // 16 * 16
+    kv = [line + n for n in (255, 256, 257, 511, 512, 513, 769)]
+    cache = Cache(gen, kv, 2, d, kind, 16, shared=[(0, len(kv), prefix)] if prefix else [])
+    q = _rand(gen, len(kv), 6, d).to(TYPES[io]).cuda()
+    cu = _i32([0, len(kv)]) if prefix else None
+    plan = api.AttnDecode(len(kv), 6, 2, d, max(kv), TYPES[io], cu_group=cu, max_prefix_len=prefix)
+    plan.workspace.fill_(0xFF)
+    o = plan.run(cache.layer(), q, _i32(kv), _i32([prefix]) if prefix else None)
+    torch.cuda.synchronize()
+    assert int(cache.err) == 0
+    _check(o, _ref(q, cache, d), d, io == "bf16", f"own keys behind {prefix}, {kind}")
+
+
+@pytest.mark.parametrize("io,kind", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_more_groups_than_a_wave_reads_at_once(io, kind):
+    """150 groups (64 are read at a time) of one to three sequences, with prefixes of many lengths."""
+    gen = torch.Generator().manual_seed(73)
+    sizes = [1 + i % 3 for i in range(150)]
+    starts = np.concatenate([[0], np.cumsum(sizes)])
+    prefix = [16 * (1 + 7 * i % 20) - (i % 5 == 4) * 3 for i in range(150)]
+    kv = [p + 1 + (11 * j + i) % 40 for i, (n, p) in enumerate(zip(sizes, prefix)) for j in range(n)]
+    shared = [(int(a), n, p) for a, n, p in zip(starts, sizes, prefix)]
+    cache = Cache(gen, kv, 2, 64, kind, 16, shared=shared)
+    q = _rand(gen, len(kv), 4, 64).to(TYPES[io]).cuda()
+    plan = api.AttnDecode(len(kv), 4, 2, 64, max(kv), TYPES[io], cu_group=_i32(starts), max_prefix_len=max(prefix))
+    plan.workspace.fill_(0xFF)
+    o = plan.run(cache.layer(), q, _i32(kv), _i32(prefix))
+    torch.cuda.synchronize()
+    assert int(cache.err) == 0
+    _check(o, _ref(q, cache, 64), 64, io == "bf16", f"150 groups, {kind}")
+
+
+@pytest.mark.parametrize("io,kind,d", [("bf16", "fp8", 128), ("f32", "f32", 64)])
+@pytest.mark.parametrize("most", [1, 4, 8])
+def test_sequences_behind_max_group(io, kind, d, most):
+    """A group larger than its plan says: the sequences behind read their whole keys themselves."""
+    gen = torch.Generator().manual_seed(74)
+    kv = [300 + 7 * i for i in range(9)]
+    cache = Cache(gen, kv, 2, d, kind, 16, shared=[(0, 9, 288)])
+    q = _rand(gen, 9, 16, d).to(TYPES[io]).cuda()
+    plan = api.AttnDecode(9, 16, 2, d, max(kv), TYPES[io], cu_group=_i32([0, 9]), max_prefix_len=288, max_group=most)
+    plan.workspace.fill_(0xFF)
+    o = plan.run(cache.layer(), q, _i32(kv), _i32([288]))
+    torch.cuda.synchronize()
+    _check(o, _ref(q, cache, d), d, io == "bf16", f"max_group {most}, {kind}")
