@@ -543,7 +543,8 @@ size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv
  * la_kv_write - new keys and values into the cache: k, v [n_tokens, kv_heads,
  * head_dim] in io_dtype (token strides as in la_attn_shape), sequence i at
  * rows cu_seqlens[i] .. cu_seqlens[i+1]-1; its tokens become keys kv_len[i] -
- * (cu[i+1] - cu[i]) .. kv_len[i] - 1.  An 8-bit cache holds x / scale rounded
+ * (cu[i+1] - cu[i]) .. kv_len[i] - 1.  Rows before cu[0] and from cu[n_seqs] on
+ * are not written, so a part of a batch's sequences serves.  An 8-bit cache holds x / scale rounded
  * to nearest even, values beyond +-448 at +-448, NaN as NaN.  A position
  * below zero or past the table counts in err_count and is not written.
  */

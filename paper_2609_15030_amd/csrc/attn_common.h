@@ -252,24 +252,4 @@ __device__ inline int wave_scan(int x) {
     return x;
 }
 
-// The sequence of item r when lane's sequence i has items(i): in steps of 64
-// sequences.  Returns the sequence, its lane in the step and the items before it.
-template <typename F>
-__device__ inline bool item_of(int n, int r, F items, int *seq, int *local) {
-    const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int x = wave_scan(i0 + lane < n ? items(i0 + lane) : 0);
-        const uint64_t past = __ballot(before + x > r);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            *seq = i0 + at;
-            *local = r - before - (at ? __builtin_amdgcn_readlane(x, at - 1) : 0);
-            return true;
-        }
-        before += __builtin_amdgcn_readlane(x, 63);
-    }
-    return false;
-}
-
 }  // namespace la

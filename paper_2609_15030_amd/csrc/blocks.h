@@ -421,7 +421,24 @@ struct KvWriteArgs {
 
 constexpr int kWriteTokens = 4;    // tokens a workgroup writes, one for each wave
 
-// Eight values to e4m3: beyond the largest finite value they become it, NaN stays.
+// The sequence of row `tok`, by offsets cu [n + 1], one sequence a lane; its rows are
+// [*first, *end).  False for rows before the first sequence and behind the last.
+__device__ inline bool sequence_of(const int32_t *cu, int n, int tok, int *seq, int *first, int *end) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = min(i0 + lane, n - 1), c0 = cu[i], c1 = cu[i + 1];
+        const uint64_t past = __ballot(c1 > tok);
+        if (!past) continue;
+        const int at = __builtin_ctzll(past);
+        *seq = i0 + at;
+        *first = __builtin_amdgcn_readlane(c0, at);
+        *end = __builtin_amdgcn_readlane(c1, at);
+        return *first <= tok;
+    }
+    return false;
+}
+
+// Four values to e4m3: beyond the largest finite value they become it, NaN stays.
 __device__ inline uint32_t fp8_of4(const float *x) {
     float y[4];
 #pragma unroll
@@ -440,9 +457,9 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t tok = a.first_token + (int64_t)blockIdx.x * kWriteTokens + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (tok >= a.n_tokens) return;
-    int seq, local;
-    if (!item_of(a.n_seqs, (int)tok, [&](int i) { return a.cu[i + 1] - a.cu[i]; }, &seq, &local)) return;
-    const int pos = a.kv_len[seq] - (a.cu[seq + 1] - a.cu[seq]) + local;
+    int seq, first, end;
+    if (!sequence_of(a.cu, a.n_seqs, (int)tok, &seq, &first, &end)) return;
+    const int pos = a.kv_len[seq] - (end - (int)tok);
     const int64_t j = pos >> a.bt_shift;
     const int id = pos >= 0 && j < a.max_blocks ? a.table[seq * a.max_blocks + j] : -1;
     if ((uint32_t)id >= (uint32_t)a.n_blocks) {
