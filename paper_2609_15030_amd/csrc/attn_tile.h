@@ -143,12 +143,20 @@ __device__ inline bool prefix_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     t->hi = min(t->keys, t->lo + kPrefixPart);
     if (t->row0 >= t->n_rows || t->lo >= t->hi) return false;
     const int first = a.by_group(t->row0), last = a.by_group(min(t->row0 + ROWS, t->n_rows) - 1);
-    int least = t->keys;
-    for (int s = first + (int)(threadIdx.x & 63); s <= last; s += 64) least = min(least, a.kv_len[s0 + s]);
+    int least = t->keys, most = 0;
+    for (int s = first + (int)(threadIdx.x & 63); s <= last; s += 64) {
+        const int len = a.kv_len[s0 + s];
+        least = min(least, len);
+        most = max(most, len);
+    }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
+    for (int d = 1; d < 64; d <<= 1) {
+        least = min(least, __shfl_xor(least, d));
+        most = max(most, __shfl_xor(most, d));
+    }
     t->all_see = max(0, __builtin_amdgcn_readfirstlane(least));
-    return true;
+    t->hi = min(t->hi, __builtin_amdgcn_readfirstlane(most));      // keys that no row sees are not read: their blocks may be gone
+    return t->lo < t->hi;
 }
 
 // The work of a prompt call's item.  One load of the lengths serves a step of 64

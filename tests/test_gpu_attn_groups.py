@@ -96,3 +96,23 @@ def test_sequences_behind_max_group(io, kind, d, most):
     o = plan.run(cache.layer(), q, _i32(kv), _i32([288]))
     torch.cuda.synchronize()
     _check(o, _ref(q, cache, d), d, io == "bf16", f"max_group {most}, {kind}")
+
+
+@pytest.mark.parametrize("io,kind", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_a_prefix_length_past_its_members(io, kind):
+    """Slots of a batch that are out of use (no key, no block) beside a prefix length
+    that is still there, and members that end before it: keys that no sequence sees
+    are neither read nor counted as missing."""
+    gen = torch.Generator().manual_seed(75)
+    kv, d = [0, 0, 0, 300, 310, 100, 90, 257, 256], 64
+    cache = Cache(gen, kv, 2, d, kind, 16, shared=[(3, 2, 288), (5, 2, 90)])
+    q = _rand(gen, len(kv), 8, d).to(TYPES[io]).cuda()
+    plan = api.AttnDecode(len(kv), 8, 2, d, 310, TYPES[io], cu_group=_i32([0, 3, 5, 7, 9]), max_prefix_len=288)
+    plan.workspace.fill_(0xFF)
+    cache.table[8] = cache.table[7]                  # the last group: one block is seen by its first member alone
+    cache.table_dev.copy_(cache.table)
+    o = plan.run(cache.layer(), q, _i32(kv), _i32([288, 288, 288, 257]))
+    torch.cuda.synchronize()
+    assert int(cache.err) == 0
+    assert not bool(o[:3].any())
+    _check(o, _ref(q, cache, d), d, io == "bf16", f"prefix lengths past their members, {kind}")
