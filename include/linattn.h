@@ -441,7 +441,8 @@ la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const i
  * sees no key (or whose every score is -inf) has o = 0; keys and values that
  * it does not see have no effect on it, infinities and NaN included (one
  * exception: an infinite value with a weight that rounds to zero gives
- * infinity or NaN).  Scores, maxima and sums are fp32 (a token with a score past
+ * infinity or NaN).  Values are summed before the division: beyond 2^120 / keys
+ * the sums may overflow.  Scores, maxima and sums are fp32 (a token with a score past
  * fp32's range has NaN); with bf16 inputs the
  * weights p_j are rounded to bf16 for the product with v.  The same call
  * gives the same bits.  A single token's result does not depend on the other
@@ -532,7 +533,10 @@ typedef struct la_prefix_groups {
  * call can be replayed after they change, up to max_kv_len (a longer kv_len is
  * cut there and counts in err_count) and max_prefix_len.  groups: NULL when
  * nothing is shared.  workspace: la_attn_decode_workspace_bytes(shape,
- * max_kv_len, max_prefix_len) bytes; nothing in it has to start at zero.
+ * max_kv_len, max_prefix_len) bytes; nothing in it has to start at zero.  It
+ * holds head_dim + 2 floats for every row and 256 keys of max_kv_len (and of
+ * max_prefix_len), however long the sequences are: 1.1 GB for 256 sequences of
+ * 64 heads of 128 at 32,768.
  */
 la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, const void *q,
                          const int32_t *kv_len_dev, int64_t max_kv_len, const la_prefix_groups *groups,
@@ -590,12 +594,14 @@ la_status la_blocks_fork(const la_block_pool *pool, const int32_t *parent_rows_d
                          const int32_t *len_dev, int64_t n, void *stream);
 
 /* la_blocks_extend - every missing entry of row rows[i] below
- * ceil(len[i] / block_tokens) gets a fresh block.  Rows are distinct. */
+ * ceil(len[i] / block_tokens) gets a fresh block.  Rows are distinct.  Its time
+ * grows with n * max_blocks (4 us for 840 entries, 73 for 131,072). */
 la_status la_blocks_extend(const la_block_pool *pool, const int32_t *rows_dev, const int32_t *len_dev,
                            int64_t n, void *stream);
 
 /* la_blocks_free - empties rows; blocks that no entry names any more go on
- * the free list, ids ascending. */
+ * the free list, ids ascending.  Its time grows with n_blocks (6 us for 3,000,
+ * 171 for 1,048,576). */
 la_status la_blocks_free(const la_block_pool *pool, const int32_t *rows_dev, int64_t n, void *stream);
 
 /* la_blocks_compact - moves the L live blocks into ids 0 .. L-1: the k-th live

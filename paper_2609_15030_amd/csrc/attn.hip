@@ -244,7 +244,9 @@ la_status check_qo(const la_attn_shape *s, const void *q, const void *o, la::Att
 
 // --- decode ------------------------------------------------------------------
 
-constexpr int kRowsGrid = 512;         // workgroups for own keys: two on every CU
+// Workgroups for own keys: two on every CU.  Those of shared prefixes come on top and
+// start first; the own keys' follow as they end.
+constexpr int kRowsGrid = 512;
 
 struct DecodePlan {
     int own_parts, prefix_parts;

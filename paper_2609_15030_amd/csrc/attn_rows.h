@@ -10,9 +10,10 @@
 // end.
 //
 // Many long sequences are bound by memory: 96 of 1 to 32,768 keys, 4 key heads of
-// 128 in 8 bits, 64.5 us at 4.9 TB/s (a large copy reaches 5.1), their join 5.4.  A
-// single one is a chain (lengths -> table -> keys -> join): 3,584 keys, 2 heads,
-// 7.4 us, its join 2.7.  64 sequences behind 6,144 shared keys: 23.5 us, of which
+// 128 in 8 bits, 66 us at 4.8 TB/s (a large copy reaches 5.1), their join 5.6; whole
+// calls of 64 of 8,000 in bf16 207 us at 5.1, in 8 bits 131 at 4.0, of 64 of 4,000 with
+// 8 key heads in fp32 378 at 5.5.  A single one is a chain (lengths -> table -> keys -> join): 3,584 keys, 2 heads,
+// 7.5 us, its join 2.6.  64 sequences behind 6,144 shared keys: 22.9 us, of which
 // memory alone would take 9.5; a prefix part is a chain of four key tiles.
 #pragma once
 #include "attn_tile.h"

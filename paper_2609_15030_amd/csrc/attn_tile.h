@@ -252,7 +252,7 @@ __device__ inline void add_nonfinite(const AttnArgs &a, const int32_t *table_row
 // fp32: key tiles of 32 keys, double buffered, and two more in flight in registers,
 // so that a tile's loads have two tiles' time to arrive.  Bound by the matrix unit
 // where a call fills the chip (8,192 tokens x 8 heads x 64: 101 TFLOP/s of the 154
-// that a large product reaches), by the uneven tiles of its parts where it does
+// that a large product reaches; suffixes of 16 prompts over a cache, 8 heads x 128: 111), by the uneven tiles of its parts where it does
 // not (1,791 + 640 + 257 tokens: 61 us, 62 TFLOP/s).  At 32 keys and 64 dims four
 // workgroups share a CU; at 64 keys two did (66 us).
 //

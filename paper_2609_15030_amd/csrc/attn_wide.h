@@ -5,8 +5,9 @@
 // (16 a wave, as in attn_tile.h, is bound by LDS: 579 against 956 TFLOP/s for
 // 32,768 tokens; 64 rows a wave leave one wave a SIMD, whose own exponentials
 // then wait for its products: 860).  As it stands the kernel takes that prompt at
-// 1,032 TFLOP/s (a product of 8,192 x 8,192 x 8,192: 1,200) and the suffixes of 16
-// prompts over an 8-bit cache at 913.
+// 1,025 to 1,048 TFLOP/s, from card to card (a product of 8,192 x 8,192 x 8,192:
+// 1,177 to 1,200), the suffixes of 16 prompts over an 8-bit cache at 893 to 923 and
+// over a bf16 one at 882 to 896.
 //
 // A row's chain is scores -> maximum -> weights -> product with V.  A wave runs it
 // as a pipeline of half tiles (32 keys): while the weights of half h are formed,

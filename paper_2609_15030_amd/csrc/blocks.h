@@ -5,12 +5,17 @@
 // last block that its tokens end inside); beside that 4 bytes for each table entry
 // and block id.  Copies run at the rate of a large copy (5.0 TB/s) once they are
 // many; small calls are bound by their launches and by chains of loads (row ->
-// table entry -> id), which is why a call is few kernels and each thread's loads
-// are independent.  Measured, in us: 64 forks of 517 to 3,584 tokens with their 64
-// children freed 16.2 (fork_take 2.9, fork 6.5, free_rows 3, free_push 2.6); 16
-// rows of 17 to 3,328 tokens with four freed, compacted and grown
-// again 49.5 (rank 4.9, move 28 at 4.9 TB/s, extend 6, free 6).  Freeing in one workgroup
-// instead of two kernels took 9 to 25: one CU's atomics are too slow.
+// table entry -> id), which is why a call is few kernels and a thread's loads
+// within one pass are independent.  Measured, in us: 64 forks of 517 to 3,584 tokens
+// with their 64 children freed 16.3 (fork_take 3, fork 7, free_rows 4, free_push 2.7);
+// 16 rows of 17 to 3,328 tokens with four freed, compacted and grown
+// again 49.9 (rank 5, move 28 at 4.9 TB/s, extend 6.5, free_rows 4, free_push 4.7).
+// Freeing in one workgroup instead of two kernels took 9 to 25: one CU's atomics are too slow.
+//
+// Handing out and taking back in a fixed order is one workgroup's work, pass after
+// pass: extend visits every entry of its rows (4 rows of 210 entries 4.4 us, 64 of
+// 2,048 73, 256 of 2,048 286), free every id of the pool (one row freed from 3,000
+// ids 6 us, 33,000 13, 1,048,576 171, 2,097,152 350).
 //
 // Block ids live in a table [rows, max_blocks] (-1: none); ref[b] counts the
 // entries that name b; the free ids are a stack, the next one at its top.
@@ -249,7 +254,8 @@ __global__ __launch_bounds__(256) void free_rows_kernel(BlockPoolArgs p, const i
 
 // One workgroup: the marked blocks go on the stack, ids ascending.  A wave takes
 // 64 E ids at a time, 64 side by side.  E = 16 for large pools, whose passes are a
-// chain; E = 4 up to kPushSmall ids, which are one pass (2.6 us where 16 take 4.4).
+// chain; E = 4 up to kPushSmall ids, which are one pass (2.6 us where 16 take 4.4, with
+// the counts in cache; 4.7 behind a large copy).
 constexpr int kPushSmall = 4 * kBlockThreads;
 template <int E>
 __global__ __launch_bounds__(kBlockThreads) void free_push_kernel(BlockPoolArgs p) {
@@ -449,7 +455,7 @@ __device__ inline uint32_t fp8_of4(const float *x) {
 
 // A wave writes one token: 8 values of a key and a value row at a time, 16-byte
 // loads; what it needs to find the place (the sequence, its length, the block) is a
-// chain of four loads, which bounds small calls (64 tokens: 3.4 us); large ones are
+// chain of four loads, which bounds small calls (64 tokens: 3.6 us); large ones are
 // bound by memory (47,248 tokens x 8 heads x 128 into an 8-bit cache: 58 us, 5.0
 // TB/s of reads and writes, what a large copy reaches).
 template <typename T, typename C, int D>
