@@ -60,7 +60,9 @@ typedef enum la_status {
 typedef enum la_dtype {
     LA_F32 = 0,
     LA_BF16 = 1,
-    LA_FP8_E4M3 = 2               /* attention caches only                          */
+    LA_FP8_E4M3 = 2,              /* attention caches only: one scale a layer        */
+    LA_FP8_E4M3_BLOCK = 3,        /* attention caches only: e4m3 codes, and          */
+    LA_INT8_BLOCK = 4             /* integer codes, with a scale a block and head    */
 } la_dtype;
 
 typedef enum la_variant {
@@ -476,11 +478,13 @@ typedef struct la_kv_layer {
     int64_t k_offset, v_offset;      /* multiples of 16                            */
     int32_t block_tokens;            /* a power of two, 16 to 256                  */
     int32_t kv_heads, head_dim;
-    int32_t dtype;                   /* LA_BF16 or LA_FP8_E4M3 (bf16 calls), LA_F32 (fp32 calls) */
-    float k_scale, v_scale;          /* 8-bit: what a stored 1 stands for; else 1  */
+    int32_t dtype;                   /* LA_BF16 or an 8-bit type (bf16 calls), LA_F32 (fp32 calls) */
+    float k_scale, v_scale;          /* LA_FP8_E4M3: what a stored 1 stands for; else 1 */
     const int32_t *block_table;      /* device [n_seqs, max_blocks]                */
     int64_t max_blocks;
     int32_t *err_count;
+    int64_t k_scales, v_scales;      /* LA_FP8_E4M3_BLOCK, LA_INT8_BLOCK only: offsets in the block of this
+                                        layer's scales, fp32 [kv_heads] each, multiples of 4 */
 } la_kv_layer;
 
 /*
@@ -548,13 +552,119 @@ size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv
  * head_dim] in io_dtype (token strides as in la_attn_shape), sequence i at
  * rows cu_seqlens[i] .. cu_seqlens[i+1]-1; its tokens become keys kv_len[i] -
  * (cu[i+1] - cu[i]) .. kv_len[i] - 1.  Rows before cu[0] and from cu[n_seqs] on
- * are not written, so a part of a batch's sequences serves.  An 8-bit cache holds x / scale rounded
- * to nearest even, values beyond +-448 at +-448, NaN as NaN.  A position
+ * are not written, so a part of a batch's sequences serves.  A position
  * below zero or past the table counts in err_count and is not written.
+ *
+ * LA_FP8_E4M3 holds x / scale rounded to nearest even, values beyond +-448 at
+ * +-448, NaN as NaN.
+ *
+ * LA_FP8_E4M3_BLOCK and LA_INT8_BLOCK hold codes x / s rounded to nearest even,
+ * with a scale s for the keys and one for the values of each block and head,
+ * which lie in the block, so that whatever moves blocks moves them too.  With A
+ * the largest magnitude that the call writes there,
+ *   e4m3   s = the smallest power of two with A <= 448 s
+ *   int8   s = A / 127, rounded up to 8 significant bits
+ * and at least 2^-100.  Where tokens before the call's stay in the block, s is
+ * no less than the block's scale, and if it is greater their codes become
+ * code * old / s, rounded to nearest even; a block's scale that no write can
+ * have left counts as 2^-100.  Values beyond +-2^127 (infinities too) are
+ * written as +-2^127.  NaN: e4m3 holds it; int8, which cannot, holds 0 and
+ * counts in err_count.  A block is written for one sequence at a time.
  */
 la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k, int64_t k_stride,
                       const void *v, int64_t v_stride, const int32_t *cu_seqlens_dev, int32_t n_seqs,
                       int64_t n_tokens, const int32_t *kv_len_dev, void *stream);
+
+/*
+ * la_kv_read - cached keys and values back out: the keys that la_kv_write
+ * with the same lengths would write, as rows k, v of io_dtype: what each stored
+ * value stands for, rounded once.  LA_BF16 or LA_F32 from any cache but an fp32
+ * one, which gives LA_F32 alone.  Rows before cu[0] and from cu[n_seqs] on are
+ * left as they are; a position below zero or past the table, or in a block that
+ * the table does not name, counts in err_count and its row is zero.
+ */
+la_status la_kv_read(const la_kv_layer *layer, int32_t io_dtype, void *k, int64_t k_stride,
+                     void *v, int64_t v_stride, const int32_t *cu_seqlens_dev, int32_t n_seqs,
+                     int64_t n_tokens, const int32_t *kv_len_dev, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions of the queries and keys of an attention layer, before
+ * la_kv_write and la_attn_*.  The first rotary_dim dims of a head are rotary_dim / 2
+ * pairs; pair i of a token at position p is turned by p freq_i and multiplied by
+ * magnitude, in fp32, and rounded once; dims from rotary_dim on stay.
+ * --------------------------------------------------------------------- */
+
+typedef enum la_rope_layout {
+    LA_ROPE_HALVES = 0,              /* pair i: dims i and i + rotary_dim / 2       */
+    LA_ROPE_PAIRS = 1                /* pair i: dims 2 i and 2 i + 1                */
+} la_rope_layout;
+
+/* Scaling of the frequencies base^(-2 i / rotary_dim) for contexts longer than
+ * a model was trained at:
+ *   LA_ROPE_LINEAR   freq / factor
+ *   LA_ROPE_BASE     base * factor^(rotary_dim / (rotary_dim - 2))
+ *   LA_ROPE_PARTS    freq (keep + (1 - keep) / factor), with keep = (n - low) / (high - low)
+ *                    cut to [0, 1] and n = original_len freq / 2 pi, the turns that the
+ *                    pair makes over the original length (a magnitude of 0.1 ln(factor) + 1
+ *                    is often used with it) */
+typedef enum la_rope_scaling_kind {
+    LA_ROPE_UNSCALED = 0,
+    LA_ROPE_LINEAR = 1,
+    LA_ROPE_BASE = 2,
+    LA_ROPE_PARTS = 3
+} la_rope_scaling_kind;
+
+typedef struct la_rope_scaling {
+    int32_t kind;
+    double factor;                   /* > 0                                        */
+    double original_len, low, high;  /* LA_ROPE_PARTS: original_len > 0, low < high */
+} la_rope_scaling;
+
+/* la_rope_frequencies - freq_out [rotary_dim / 2], radians a token; scaling may
+ * be NULL.  Host only. */
+la_status la_rope_frequencies(int32_t rotary_dim, double base, const la_rope_scaling *scaling, double *freq_out);
+
+/* la_rope_turns - n frequencies (any finite ones) as la_rope_apply reads them:
+ * the fraction of a turn that a token adds, in units of 2^-64.  Host only. */
+la_status la_rope_turns(const double *freq, int32_t n, uint64_t *turns_out);
+
+typedef struct la_rope_plan {
+    int32_t head_dim;                /* a multiple of 8                             */
+    int32_t rotary_dim;              /* even, from 2 to head_dim, at most 512       */
+    int32_t layout;                  /* la_rope_layout                              */
+    int32_t io_dtype;                /* LA_BF16 or LA_F32                           */
+    float magnitude;
+    const uint64_t *turns_dev;       /* device [rotary_dim / 2], of la_rope_turns   */
+} la_rope_plan;
+
+/* Rows of queries or keys: x, y [n_tokens, heads, head_dim], heads of a token
+ * packed, strides in elements from one token to the next (0: packed rows), rows
+ * on 16-byte lines.  y may be x (then with its stride), else must not overlap it. */
+typedef struct la_rope_rows {
+    const void *x;
+    void *y;
+    int32_t heads;
+    int64_t x_stride, y_stride;
+} la_rope_rows;
+
+/* Where the tokens are: positions_dev, int32 [n_tokens], any values; or, where
+ * that is NULL, the positions that la_kv_write gives the same rows (rows outside
+ * every sequence are then left as they are). */
+typedef struct la_rope_positions {
+    const int32_t *positions_dev;
+    const int32_t *cu_seqlens_dev;   /* [n_seqs + 1]                                */
+    int32_t n_seqs;
+    const int32_t *kv_len_dev;       /* [n_seqs]                                    */
+} la_rope_positions;
+
+/*
+ * la_rope_apply - turns the rows of q and of k (either may be NULL) in one
+ * launch.  transpose: by the opposite angles, with the same magnitude, which is
+ * the gradient: of y's gradient it makes x's.  An angle is off by at most
+ * 2e-7 radians at any position.
+ */
+la_status la_rope_apply(const la_rope_plan *plan, const la_rope_rows *q, const la_rope_rows *k, int64_t n_tokens,
+                        const la_rope_positions *at, int32_t transpose, void *stream);
 
 /* The blocks of a cache and their book, all on the device.  table: one row
  * per request, -1 where there is no block; ref_count[b]: entries that name

@@ -215,6 +215,40 @@ class AttnDecode:
         return self.o
 
 
+class Rope:
+    """Rotary positions of heads of head_dim: the first rotary_dim dims (None:
+    all) in pairs (i, i + rotary_dim / 2) (layout "halves") or (2 i, 2 i + 1)
+    ("pairs"), at frequencies base^(-2 i / rotary_dim) under a scaling
+    (la.make_rope_scaling), or at given ones (radians a token, fp64)."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, layout: str = "halves", base: float = 10000.0,
+                 scaling: Optional[la.LaRopeScaling] = None, frequencies: Optional[np.ndarray] = None,
+                 magnitude: float = 1.0, device="cuda"):
+        self.head_dim, self.rotary_dim = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim)
+        self.layout, self.magnitude = layout, float(magnitude)
+        if frequencies is None:
+            frequencies = la.la_rope_frequencies(self.rotary_dim, base, scaling)
+        self.frequencies = np.ascontiguousarray(frequencies, np.float64)
+        self.turns = torch.from_numpy(la.la_rope_turns(self.frequencies).view(np.int64)).to(device)
+        self._plans = {}                           # by type
+
+    def apply(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+              cu_seqlens: Optional[torch.Tensor] = None, kv_len: Optional[torch.Tensor] = None, transpose: bool = False,
+              stream=None):
+        """Turns q and k [T, heads, head_dim] at positions int32 [T], or at those
+        of the sequences of cu_seqlens and kv_len (la_kv_write's); in place where no
+        output is given.  transpose: the gradient.  Returns the outputs."""
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+        dtype = (k if q is None else q).dtype
+        plan = self._plans.get(dtype)
+        if plan is None:
+            plan = self._plans[dtype] = la.make_rope_plan(self.head_dim, self.rotary_dim, self.layout, la._dtype_of(dtype),
+                                                          self.turns, self.magnitude)
+        la.la_rope_apply(plan, q, q_out, k, k_out, positions, cu_seqlens, kv_len, transpose, stream)
+        return q_out, k_out
+
+
 class BlockPool:
     """The blocks of a cache with their table, reference counts and free list
     (la_block_pool), over tensors the caller holds; BlockPool.new makes an

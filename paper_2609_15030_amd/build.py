@@ -1,8 +1,8 @@
 """Build the gfx950 shared library in-tree with hipcc.
 
 ``python -m paper_2609_15030_amd.build`` compiles csrc/linattn.hip (the
-linear-attention path) and csrc/attn.hip (attention over a cache and the
-cache's blocks), side by side, and links them into
+linear-attention path), csrc/attn.hip (attention over a cache and the
+cache's blocks) and csrc/rope.hip (rotary positions), side by side, and links them into
 paper_2609_15030_amd/liblinattn.so.  Every call compiles (no caching): the
 output is written to a temporary name and moved into place.
 """
@@ -15,7 +15,7 @@ import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRCS = [os.path.join(PKG, "csrc", f) for f in ("linattn.hip", "attn.hip")]
+SRCS = [os.path.join(PKG, "csrc", f) for f in ("linattn.hip", "attn.hip", "rope.hip")]
 LIB = os.path.join(PKG, "liblinattn.so")
 ARCH = "gfx950"
 

@@ -14,6 +14,7 @@
 #include "attn_rows.h"
 #include "attn_wide.h"
 #include "blocks.h"
+#include "kv_codes.h"
 
 namespace {
 
@@ -26,6 +27,7 @@ constexpr int64_t kMaxInt = 0x7fffffff;
 constexpr int64_t max_grid(int threads) { return 0xffffffffll / threads; }
 
 int64_t dtype_size(int32_t d) { return d == LA_F32 ? 4 : d == LA_BF16 ? 2 : 1; }
+bool block_scaled(int32_t d) { return d == LA_FP8_E4M3_BLOCK || d == LA_INT8_BLOCK; }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int shift_of(int32_t pow2) { return __builtin_ctz((unsigned)pow2); }
 
@@ -65,7 +67,7 @@ la_status token_stride(int64_t given, int64_t heads, const la_attn_shape *s, con
 
 la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
     if (!y) return fail(LA_ERR_INVALID_ARG, "layer is NULL");
-    if (y->dtype != LA_F32 && y->dtype != LA_BF16 && y->dtype != LA_FP8_E4M3)
+    if (y->dtype != LA_F32 && y->dtype != LA_BF16 && y->dtype != LA_FP8_E4M3 && !block_scaled(y->dtype))
         return fail(LA_ERR_INVALID_ARG, "cache dtype=%d", y->dtype);
     if ((y->dtype == LA_F32) != (io_dtype == LA_F32))
         return fail(LA_ERR_UNSUPPORTED, "an fp32 cache goes with fp32 queries, a bf16 or 8-bit one with bf16");
@@ -86,7 +88,17 @@ la_status check_layer(const la_kv_layer *y, int32_t io_dtype) {
     if (!(y->k_scale > 0.f) || !(y->v_scale > 0.f) || !std::isfinite(y->k_scale) || !std::isfinite(y->v_scale))
         return fail(LA_ERR_INVALID_ARG, "k_scale=%g and v_scale=%g must be positive and finite", (double)y->k_scale, (double)y->v_scale);
     if (y->dtype != LA_FP8_E4M3 && (y->k_scale != 1.f || y->v_scale != 1.f))
-        return fail(LA_ERR_INVALID_ARG, "scales other than 1 go with an 8-bit cache");
+        return fail(LA_ERR_INVALID_ARG, "k_scale and v_scale other than 1 go with an 8-bit cache of one scale");
+    if (block_scaled(y->dtype)) {
+        const int64_t size = 4 * (int64_t)y->kv_heads, ks = y->k_scales, vs = y->v_scales;
+        if (ks < 0 || vs < 0 || ks % 4 || vs % 4 || ks > y->block_bytes - size || vs > y->block_bytes - size)
+            return fail(LA_ERR_INVALID_ARG, "scales at %lld and %lld (%lld bytes each) must lie in a block of %lld bytes, on 4-byte lines",
+                        (long long)ks, (long long)vs, (long long)size, (long long)y->block_bytes);
+        auto meet = [](int64_t a, int64_t n, int64_t b, int64_t m) { return a < b + m && b < a + n; };
+        if (meet(ks, size, vs, size) || meet(ks, size, y->k_offset, part) || meet(ks, size, y->v_offset, part) ||
+            meet(vs, size, y->k_offset, part) || meet(vs, size, y->v_offset, part))
+            return fail(LA_ERR_INVALID_ARG, "scales overlap keys, values or one another in the block");
+    }
     if (y->max_blocks < 1 || y->max_blocks > 0x7fffff00 / bt)
         return fail(LA_ERR_INVALID_ARG, "max_blocks=%lld must be positive and cover fewer than 2^31 tokens", (long long)y->max_blocks);
     if (!y->block_table) return fail(LA_ERR_INVALID_ARG, "block_table is required");
@@ -113,6 +125,10 @@ la::KvSource cached(const la_kv_layer *y) {
     k.n_blocks = (int32_t)y->n_blocks;
     k.bt_shift = shift_of(y->block_tokens);
     k.err = y->err_count;
+    if (block_scaled(y->dtype)) {
+        k.ks = (const char *)y->cache + y->k_scales;
+        k.vs = (const char *)y->cache + y->v_scales;
+    }
     return k;
 }
 
@@ -229,6 +245,8 @@ la_status run_prompt(const la_attn_shape *s, la::AttnArgs &a, const la_kv_layer 
         return s->io_dtype == LA_F32 ? prompt_of_dim<float, float, false>(d, a, p, st) : prompt_of_dim<__bf16, __bf16, false>(d, a, p, st);
     if (layer->dtype == LA_F32) return prompt_of_dim<float, float, true>(d, a, p, st);
     if (layer->dtype == LA_BF16) return prompt_of_dim<__bf16, __bf16, true>(d, a, p, st);
+    if (layer->dtype == LA_FP8_E4M3_BLOCK) return prompt_of_dim<__bf16, la::e4m3_code, true>(d, a, p, st);
+    if (layer->dtype == LA_INT8_BLOCK) return prompt_of_dim<__bf16, la::int8_code, true>(d, a, p, st);
     return prompt_of_dim<__bf16, la::fp8_t, true>(d, a, p, st);
 }
 
@@ -331,6 +349,72 @@ la_status launch_kv_write(int d, la::KvWriteArgs &a, hipStream_t st) {
         else hipLaunchKernelGGL((la::kv_write_kernel<T, C, 128>), grid, dim3(256), 0, st, a);
         if (la_status e = hip_check("cache write launch")) return e;
     }
+    return LA_OK;
+}
+
+// Pieces of 8 values a lane holds of a unit, and waves that share one.
+template <typename C, int D>
+la_status launch_kv_codes(la::KvCodesArgs &a, hipStream_t st) {
+    const int pieces = D / 8 << a.w.bt_shift;                  // of a unit
+    const bool small = pieces <= 4 * 64;
+    a.team_shift = pieces <= 16 * 64 ? 0 : pieces <= 32 * 64 ? 1 : 2;
+    a.unit_groups = (int32_t)up(2 * (int64_t)a.w.kv_heads << a.team_shift, 4);
+    const int64_t groups = ((a.w.n_tokens >> a.w.bt_shift) + 2 * (int64_t)a.w.n_seqs) * a.unit_groups, step = max_grid(256);
+    for (a.first_group = 0; a.first_group < groups; a.first_group += step) {
+        const dim3 grid((unsigned)std::min(groups - a.first_group, step));
+        if (small) hipLaunchKernelGGL((la::kv_write_codes_kernel<C, D, 4>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((la::kv_write_codes_kernel<C, D, 16>), grid, dim3(256), 0, st, a);
+        if (la_status e = hip_check("cache write launch")) return e;
+    }
+    return LA_OK;
+}
+
+template <typename T, typename C>
+la_status launch_kv_read(int d, la::KvWriteArgs &a, hipStream_t st) {
+    constexpr int64_t STEP = max_grid(256) * la::kWriteTokens;
+    for (a.first_token = 0; a.first_token < a.n_tokens; a.first_token += STEP) {
+        const dim3 grid((unsigned)up(std::min(a.n_tokens - a.first_token, STEP), la::kWriteTokens));
+        if (d == 64) hipLaunchKernelGGL((la::kv_read_kernel<T, C, 64>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((la::kv_read_kernel<T, C, 128>), grid, dim3(256), 0, st, a);
+        if (la_status e = hip_check("cache read launch")) return e;
+    }
+    return LA_OK;
+}
+
+// Arguments of a call that writes or reads the rows of a layer; *n_tokens 0: nothing to do.
+la_status kv_rows_args(const la_kv_layer *layer, int32_t io_dtype, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                       const int32_t *cu_seqlens_dev, int32_t n_seqs, int64_t n_tokens, const int32_t *kv_len_dev, la::KvWriteArgs *a) {
+    if (n_seqs < 0 || n_tokens < 0 || n_tokens > 0x7fffff00)
+        return fail(LA_ERR_INVALID_ARG, "n_seqs=%d, n_tokens=%lld", n_seqs, (long long)n_tokens);
+    a->n_tokens = n_seqs == 0 ? 0 : n_tokens;
+    if (a->n_tokens == 0) return LA_OK;
+    if (!k || !v || !cu_seqlens_dev || !kv_len_dev) return fail(LA_ERR_INVALID_ARG, "k, v, cu_seqlens_dev and kv_len_dev are required");
+    if (!aligned16(k) || !aligned16(v)) return fail(LA_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+    la_attn_shape s{};
+    s.head_dim = layer->head_dim;
+    s.io_dtype = io_dtype;
+    if (la_status e = token_stride(k_stride, layer->kv_heads, &s, "k_stride", &a->k_stride)) return e;
+    if (la_status e = token_stride(v_stride, layer->kv_heads, &s, "v_stride", &a->v_stride)) return e;
+    a->k = k;
+    a->v = v;
+    a->ck = (char *)layer->cache + layer->k_offset;
+    a->cv = (char *)layer->cache + layer->v_offset;
+    if (block_scaled(layer->dtype)) {
+        a->ks = (char *)layer->cache + layer->k_scales;
+        a->vs = (char *)layer->cache + layer->v_scales;
+    }
+    a->block_bytes = layer->block_bytes;
+    a->max_blocks = layer->max_blocks;
+    a->table = layer->block_table;
+    a->cu = cu_seqlens_dev;
+    a->kv_len = kv_len_dev;
+    a->err = layer->err_count;
+    a->k_scale = layer->k_scale;
+    a->v_scale = layer->v_scale;
+    a->n_seqs = n_seqs;
+    a->kv_heads = layer->kv_heads;
+    a->n_blocks = (int32_t)layer->n_blocks;
+    a->bt_shift = shift_of(layer->block_tokens);
     return LA_OK;
 }
 
@@ -452,6 +536,8 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     (void)hipGetLastError();
     if (layer->dtype == LA_F32) return decode_of_dim<float, float>(shape->head_dim, a, blocks, st);
     if (layer->dtype == LA_BF16) return decode_of_dim<__bf16, __bf16>(shape->head_dim, a, blocks, st);
+    if (layer->dtype == LA_FP8_E4M3_BLOCK) return decode_of_dim<__bf16, la::e4m3_code>(shape->head_dim, a, blocks, st);
+    if (layer->dtype == LA_INT8_BLOCK) return decode_of_dim<__bf16, la::int8_code>(shape->head_dim, a, blocks, st);
     return decode_of_dim<__bf16, la::fp8_t>(shape->head_dim, a, blocks, st);
 }
 
@@ -460,38 +546,43 @@ la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k,
     if (io_dtype != LA_F32 && io_dtype != LA_BF16)
         return fail(LA_ERR_INVALID_ARG, "io_dtype=%d must be LA_F32 or LA_BF16", io_dtype);
     if (la_status e = check_layer(layer, io_dtype)) return e;
-    if (n_seqs < 0 || n_tokens < 0 || n_tokens > 0x7fffff00)
-        return fail(LA_ERR_INVALID_ARG, "n_seqs=%d, n_tokens=%lld", n_seqs, (long long)n_tokens);
-    if (n_tokens == 0 || n_seqs == 0) return LA_OK;
-    if (!k || !v || !cu_seqlens_dev || !kv_len_dev) return fail(LA_ERR_INVALID_ARG, "k, v, cu_seqlens_dev and kv_len_dev are required");
-    if (!aligned16(k) || !aligned16(v)) return fail(LA_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
-    la_attn_shape s{};
-    s.head_dim = layer->head_dim;
-    s.io_dtype = io_dtype;
     la::KvWriteArgs a{};
-    if (la_status e = token_stride(k_stride, layer->kv_heads, &s, "k_stride", &a.k_stride)) return e;
-    if (la_status e = token_stride(v_stride, layer->kv_heads, &s, "v_stride", &a.v_stride)) return e;
-    a.k = k;
-    a.v = v;
-    a.ck = (char *)layer->cache + layer->k_offset;
-    a.cv = (char *)layer->cache + layer->v_offset;
-    a.block_bytes = layer->block_bytes;
-    a.max_blocks = layer->max_blocks;
-    a.n_tokens = n_tokens;
-    a.table = layer->block_table;
-    a.cu = cu_seqlens_dev;
-    a.kv_len = kv_len_dev;
-    a.err = layer->err_count;
-    a.k_scale = layer->k_scale;
-    a.v_scale = layer->v_scale;
-    a.n_seqs = n_seqs;
-    a.kv_heads = layer->kv_heads;
-    a.n_blocks = (int32_t)layer->n_blocks;
-    a.bt_shift = shift_of(layer->block_tokens);
+    if (la_status e = kv_rows_args(layer, io_dtype, k, k_stride, v, v_stride, cu_seqlens_dev, n_seqs, n_tokens, kv_len_dev, &a)) return e;
+    if (a.n_tokens == 0) return LA_OK;
+    hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
-    if (layer->dtype == LA_F32) return launch_kv_write<float, float>(layer->head_dim, a, (hipStream_t)stream);
-    if (layer->dtype == LA_BF16) return launch_kv_write<__bf16, __bf16>(layer->head_dim, a, (hipStream_t)stream);
-    return launch_kv_write<__bf16, la::fp8_t>(layer->head_dim, a, (hipStream_t)stream);
+    if (block_scaled(layer->dtype)) {
+        la::KvCodesArgs c{};
+        c.w = a;
+        const bool d64 = layer->head_dim == 64;
+        if (layer->dtype == LA_INT8_BLOCK) return d64 ? launch_kv_codes<la::int8_code, 64>(c, st) : launch_kv_codes<la::int8_code, 128>(c, st);
+        return d64 ? launch_kv_codes<la::e4m3_code, 64>(c, st) : launch_kv_codes<la::e4m3_code, 128>(c, st);
+    }
+    if (layer->dtype == LA_F32) return launch_kv_write<float, float>(layer->head_dim, a, st);
+    if (layer->dtype == LA_BF16) return launch_kv_write<__bf16, __bf16>(layer->head_dim, a, st);
+    return launch_kv_write<__bf16, la::fp8_t>(layer->head_dim, a, st);
+}
+
+la_status la_kv_read(const la_kv_layer *layer, int32_t io_dtype, void *k, int64_t k_stride, void *v, int64_t v_stride,
+                     const int32_t *cu_seqlens_dev, int32_t n_seqs, int64_t n_tokens, const int32_t *kv_len_dev, void *stream) {
+    if (io_dtype != LA_F32 && io_dtype != LA_BF16)
+        return fail(LA_ERR_INVALID_ARG, "io_dtype=%d must be LA_F32 or LA_BF16", io_dtype);
+    // an fp32 cache goes with fp32 rows; the others are read as either
+    if (la_status e = check_layer(layer, layer && layer->dtype != LA_F32 ? LA_BF16 : io_dtype)) return e;
+    la::KvWriteArgs a{};
+    if (la_status e = kv_rows_args(layer, io_dtype, k, k_stride, v, v_stride, cu_seqlens_dev, n_seqs, n_tokens, kv_len_dev, &a)) return e;
+    if (a.n_tokens == 0) return LA_OK;
+    hipStream_t st = (hipStream_t)stream;
+    (void)hipGetLastError();
+    const int d = layer->head_dim;
+    const bool f32 = io_dtype == LA_F32;
+    switch (layer->dtype) {
+    case LA_F32: return launch_kv_read<float, float>(d, a, st);
+    case LA_BF16: return f32 ? launch_kv_read<float, __bf16>(d, a, st) : launch_kv_read<__bf16, __bf16>(d, a, st);
+    case LA_FP8_E4M3: return f32 ? launch_kv_read<float, la::fp8_t>(d, a, st) : launch_kv_read<__bf16, la::fp8_t>(d, a, st);
+    case LA_FP8_E4M3_BLOCK: return f32 ? launch_kv_read<float, la::e4m3_code>(d, a, st) : launch_kv_read<__bf16, la::e4m3_code>(d, a, st);
+    default: return f32 ? launch_kv_read<float, la::int8_code>(d, a, st) : launch_kv_read<__bf16, la::int8_code>(d, a, st);
+    }
 }
 
 la_status la_blocks_copy(const la_block_pool *pool, const int32_t *src_ids_dev, const int32_t *dst_ids_dev, int64_t n, void *stream) {

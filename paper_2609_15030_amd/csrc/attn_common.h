@@ -17,11 +17,23 @@
 // q) are the B operand of O^T = V^T P^T as they stand: a lane's accumulators
 // belong to one q row, and the contraction index is permuted on the V side.
 #pragma once
+#include <type_traits>
+
 #include "la_common.h"
 
 namespace la {
 
 typedef unsigned char fp8_t;               // e4m3 bits
+// Codes of a cache whose blocks hold a scale for each key head: a code stands for
+// itself times the scale.
+struct e4m3_code { unsigned char bits; };  // scales: powers of two
+struct int8_code { signed char bits; };
+template <typename C> constexpr bool kBlockScaled = std::is_same<C, e4m3_code>::value || std::is_same<C, int8_code>::value;
+// Where attention applies the scales.  A power of two goes into the conversion to bf16,
+// exactly and for nothing.  Others would round there: those of keys multiply the scores
+// and those of values the weights, in fp32 (before the weights' own rounding to bf16).
+template <typename C> constexpr bool kScaleCodes = std::is_same<C, e4m3_code>::value;
+template <typename C> constexpr bool kScaleScores = kBlockScaled<C> && !kScaleCodes<C>;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -37,6 +49,7 @@ struct KvSource {
     int64_t max_blocks;
     int32_t n_blocks, bt_shift;    // blocks of 2^bt_shift tokens
     int32_t *err;
+    const char *ks, *vs;           // block-scaled cache: the layer's scales in block 0, fp32 [kv_heads]
 };
 
 // Division of n < 2^31 by a divisor known to the host: a high product, an add and
@@ -105,25 +118,30 @@ __device__ inline uint2 buf_load8(__amdgpu_buffer_rsrc_t r, uint32_t voff) {
     return make_uint2((uint32_t)v[0], (uint32_t)v[1]);
 }
 
-// Four e4m3 values as bf16 pairs (exact).
-__device__ inline uint2 bf16_of_fp8(uint32_t x) {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false);
-    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true);
+// Four codes as bf16 pairs, exactly; e4m3 times a power of two.
+template <typename C> __device__ inline uint2 bf16_of4(uint32_t x, float scale = 1.0f) {
+    bf16x2 a, b;
+    if constexpr (std::is_same<C, int8_code>::value) {
+        a = bf16x2{(__bf16)(float)(int8_t)x, (__bf16)(float)(int8_t)(x >> 8)};
+        b = bf16x2{(__bf16)(float)(int8_t)(x >> 16), (__bf16)(float)(int8_t)(x >> 24)};
+    } else {
+        a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
+        b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+    }
     return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
 }
 
 // The registers of one piece in flight: 16 bytes, or 8 that become 16.
-template <typename C> struct Raw { uint4 x; };
-template <> struct Raw<fp8_t> { uint2 x; };
+template <typename C> struct Raw { std::conditional_t<sizeof(C) == 1, uint2, uint4> x; };
 
 template <typename C> __device__ inline Raw<C> load_piece(__amdgpu_buffer_rsrc_t r, uint32_t voff) {
     if constexpr (sizeof(C) == 1) return {buf_load8(r, voff)};
     else return {buf_load16(r, voff, 0)};
 }
 
-template <typename C> __device__ inline uint4 piece_of(const Raw<C> &p) {
+template <typename C> __device__ inline uint4 piece_of(const Raw<C> &p, float scale = 1.0f) {
     if constexpr (sizeof(C) == 1) {
-        const uint2 a = bf16_of_fp8(p.x.x), b = bf16_of_fp8(p.x.y);
+        const uint2 a = bf16_of4<C>(p.x.x, scale), b = bf16_of4<C>(p.x.y, scale);
         return make_uint4(a.x, a.y, b.x, b.y);
     } else {
         return p.x;
@@ -167,6 +185,7 @@ constexpr int kRunTokens = 16;
 struct Runs {
     int64_t at;
     uint64_t bad;
+    float ks, vs;                  // block-scaled cache: the lane's run's scales
     // The lane's block id of the 1,024 tokens `ahead` of base.  Compared by distance: a
     // sequence may end so near 2^31 that the token itself passes it.
     __device__ static inline int fetch(const KvSource &s, const int32_t *table_row, int base, int ahead, int hi) {
@@ -181,6 +200,18 @@ struct Runs {
         at = (int64_t)(ok ? id : 0) * s.block_bytes +
              (int64_t)((kvh << s.bt_shift) + (int)(t & ((1u << s.bt_shift) - 1))) * row_bytes;    // may pass 2 GB within a block
     }
+    // Scales of the lane's run, of block `id` (as fetched `ahead` of base); 1 past the last
+    // key and in blocks that are none, whose bytes may be anything.
+    __device__ static inline void fetch_scales(const KvSource &s, int id, int base, int ahead, int hi, int kvh, float *ks, float *vs) {
+        *ks = *vs = 1.f;
+        if (ahead + kRunTokens * (int)(threadIdx.x & 63) < hi - base && (uint32_t)id < (uint32_t)s.n_blocks) {
+            const int64_t b = (int64_t)id * s.block_bytes + 4 * (int64_t)kvh;
+            *ks = *(const float *)(s.ks + b);
+            *vs = *(const float *)(s.vs + b);
+        }
+    }
+    __device__ inline float k_scale(int r) const { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), r)); }
+    __device__ inline float v_scale(int r) const { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), r)); }
     __device__ inline int64_t run(int r) const {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r);
         const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), r);
@@ -188,6 +219,10 @@ struct Runs {
     }
     __device__ inline bool named(int r) const { return !(bad >> r & 1); }
 };
+
+// What the scores of a run with key scale ks are multiplied by.  Not zero: masked scores
+// are minus infinity when they are multiplied.
+__device__ inline float run_factor(float c, float ks) { return fmaxf(c * ks, 0x1p-126f); }
 
 // Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a
 // q row of a 16-column accumulator.
@@ -250,6 +285,23 @@ __device__ inline int wave_scan(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // row ends to the next row, then to the upper half
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
     return x;
+}
+
+// The sequence of row `tok`, by offsets cu [n + 1], one sequence a lane; its rows are
+// [*first, *end).  False for rows before the first sequence and behind the last.
+__device__ inline bool sequence_of(const int32_t *cu, int n, int tok, int *seq, int *first, int *end) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = min(i0 + lane, n - 1), c0 = cu[i], c1 = cu[i + 1];
+        const uint64_t past = __ballot(c1 > tok);
+        if (!past) continue;
+        const int at = __builtin_ctzll(past);
+        *seq = i0 + at;
+        *first = __builtin_amdgcn_readlane(c0, at);
+        *end = __builtin_amdgcn_readlane(c1, at);
+        return *first <= tok;
+    }
+    return false;
 }
 
 }  // namespace la

@@ -130,7 +130,9 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         // the part's runs of 16 keys, one a lane
         static_assert(kOwnPart <= 64 * kRunTokens, "a lane for each run");
         Runs runs;
-        runs.set(a.kv, Runs::fetch(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo, 0, hi), lo, kvh, RB);
+        const int run_id = Runs::fetch(a.kv, a.kv.table + (int64_t)seq * a.kv.max_blocks, lo, 0, hi);
+        runs.set(a.kv, run_id, lo, kvh, RB);
+        if constexpr (kBlockScaled<C>) Runs::fetch_scales(a.kv, run_id, lo, 0, hi, kvh, &runs.ks, &runs.vs);
         uint4 qf[NQ];
         {
             const T *qp = (const T *)a.q + seq * a.q_stride + (int64_t)head * D;
@@ -166,6 +168,19 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
         auto compute = [&](int t0, const Flight &f) {
             if (t0 >= hi) return;
             f32x4 s[NT];
+            float ks[NT] = {}, vs[NT] = {};                    // scales of the tile's runs
+            if constexpr (kBlockScaled<C>) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int r = ((t0 - lo) / kRunTokens + n) & 63;
+                    ks[n] = runs.k_scale(r);
+                    vs[n] = runs.v_scale(r);
+                }
+            }
+            auto bf16_of = [&](uint32_t y, float scale) {      // of a key's or value's four codes
+                if constexpr (kScaleCodes<C>) return bf16_of4<C>(y, scale);
+                else return bf16_of4<C>(y);
+            };
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 s[n] = zero4();
@@ -173,7 +188,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
                 for (int k = 0; k < NK; ++k) {
                     const uint4 x = f.k[n][k];
                     if constexpr (F8) {
-                        const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
+                        const uint2 e0 = bf16_of(x.x, ks[n]), e1 = bf16_of(x.y, ks[n]), e2 = bf16_of(x.z, ks[n]), e3 = bf16_of(x.w, ks[n]);
                         s[n] = M::mma(__builtin_bit_cast(bf16x8, make_uint4(e0.x, e0.y, e1.x, e1.y)),
                                       __builtin_bit_cast(bf16x8, qf[2 * k]), s[n]);
                         s[n] = M::mma(__builtin_bit_cast(bf16x8, make_uint4(e2.x, e2.y, e3.x, e3.y)),
@@ -197,7 +212,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
                     // keys that the prefix's part has: a weight of zero would not undo an infinity
                     if (t0 < first && t0 + row < first) x = make_uint4(0, 0, 0, 0);
                     if constexpr (F8) {
-                        const uint2 e0 = bf16_of_fp8(x.x), e1 = bf16_of_fp8(x.y), e2 = bf16_of_fp8(x.z), e3 = bf16_of_fp8(x.w);
+                        const uint2 e0 = bf16_of(x.x, vs[n]), e1 = bf16_of(x.y, vs[n]), e2 = bf16_of(x.z, vs[n]), e3 = bf16_of(x.w, vs[n]);
                         to[2 * (lane % VPR)] = make_uint4(e0.x, e0.y, e1.x, e1.y);
                         to[2 * (lane % VPR) + 1] = make_uint4(e2.x, e2.y, e3.x, e3.y);
                     } else {
@@ -207,15 +222,18 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
             const bool masked = t0 < first || t0 + KT > hi;
             float top = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                float c = a.c;
+                if constexpr (kScaleScores<C>) c = run_factor(c, ks[n]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float x = s[n][i] * a.c;
+                    float x = s[n][i] * c;
                     const int tok = t0 + 16 * n + 4 * g + i;
                     if (masked && (tok < first || tok >= hi)) x = -INFINITY;
                     s[n][i] = x;
                     top = fmaxf(top, x);
                 }
+            }
             const float m2 = fmaxf(m, row_max16(top));
             const float mu = m2 == -INFINITY ? 0.f : m2;
             const float shrink = __builtin_amdgcn_exp2f(m - mu);
@@ -227,6 +245,7 @@ __device__ __forceinline__ void rows_run(const AttnArgs &a, int b, int n_blocks,
                 for (int i = 0; i < 4; ++i) {
                     s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - mu);
                     l += s[n][i];
+                    if constexpr (kScaleScores<C>) s[n][i] *= vs[n];
                 }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -317,7 +336,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_decode_kernel(AttnArgs a
     constexpr int ROWS = WIDE ? kPromptRows : kTileRows;
     static_assert(kRowsThreads == kWideThreads && kRowsThreads == kTileThreads, "one launch for both");
     __shared__ union Lds {
-        std::conditional_t<WIDE, WideLds<D>, TileLds<D>> tile;
+        std::conditional_t<WIDE, WideLds<C, D>, TileLds<D>> tile;
         RowsLds<T, D> rows;
     } sm;
     if ((int)blockIdx.x < a.prefix_items) {

@@ -19,7 +19,9 @@ namespace la {
 template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvLoads {
     static constexpr int STEP = NW * RPL;        // rows from one run of a wave to the next
     static_assert(STEP % kRunTokens == 0 || kRunTokens % STEP == 0, "a wave's rows lie in one run of 16");
-    struct Place {
+    struct Scales { float k[LOADS], v[LOADS]; };
+    struct None {};
+    struct Place : std::conditional_t<kScaleCodes<C>, Scales, None> {
         int64_t at[LOADS];
         uint32_t missing;
     };
@@ -28,6 +30,8 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
     int kvh, hi, wave;
     Runs runs;
     int base, next;                              // first token of `runs`; the lane's block id of the 1,024 tokens behind
+    float next_ks, next_vs;                      // their scales: loaded at the first tile after `next`, so that no tile waits for either
+    bool ahead;
 
     __device__ inline void begin(const KvSource &s, int lo) {
         if constexpr (PAGED) {
@@ -35,6 +39,10 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
             const int id = Runs::fetch(s, table_row, base, 0, hi);
             next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
             runs.set(s, id, base, kvh, RB);
+            if constexpr (kBlockScaled<C>) {
+                Runs::fetch_scales(s, id, base, 0, hi, kvh, &runs.ks, &runs.vs);
+                ahead = false;
+            }
         }
     }
     // The place of tile t0; tiles come in order.
@@ -44,6 +52,14 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
                 base += 64 * kRunTokens;
                 runs.set(s, next, base, kvh, RB);
                 next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
+                if constexpr (kBlockScaled<C>) {
+                    runs.ks = next_ks;
+                    runs.vs = next_vs;
+                    ahead = false;
+                }
+            } else if (kBlockScaled<C> && !ahead && t0 > base) {
+                Runs::fetch_scales(s, next, base, 64 * kRunTokens, hi, kvh, &next_ks, &next_vs);
+                ahead = true;
             }
             const int r0 = ((t0 - base) + wave * RPL) / kRunTokens;
             p->missing = 0;
@@ -53,6 +69,13 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
             }
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) p->at[i] = runs.run(r0 + i * STEP / kRunTokens) + i * STEP % kRunTokens * RB;
+            if constexpr (kScaleCodes<C>) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) {
+                    p->k[i] = runs.k_scale(r0 + i * STEP / kRunTokens);
+                    p->v[i] = runs.v_scale(r0 + i * STEP / kRunTokens);
+                }
+            }
         }
     }
     // A lane's byte offset within its run, from its row of the RPL and piece.
@@ -71,10 +94,11 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
             for (int i = 0; i < LOADS; ++i) f[i] = load_piece<C>(res, voff + (uint32_t)((NW * i + wave) * RPL) * (uint32_t)stride);
         }
     }
-    // Run i's piece as it goes to LDS.
-    __device__ static inline uint4 piece(const Raw<C> &f, const Place &p, int i) {
+    // Run i's piece of keys or values as it goes to LDS.
+    __device__ static inline uint4 piece(const Raw<C> &f, const Place &p, int i, bool values = false) {
         if (PAGED && p.missing && (p.missing >> i & 1)) return make_uint4(0, 0, 0, 0);
-        return piece_of<C>(f);
+        if constexpr (kScaleCodes<C>) return piece_of<C>(f, values ? p.v[i] : p.k[i]);
+        else return piece_of<C>(f);
     }
 };
 
@@ -212,8 +236,8 @@ __device__ inline bool prompt_tile_of(const AttnArgs &a, uint32_t b, RowTile *t)
     return false;
 }
 
-// Stored values of v at token `tok`, dims d .. d + 3, of one key head (zero in a
-// block that the table does not name).
+// Stored values of v at token `tok`, dims d .. d + 3, of one key head, without a block's
+// scale (zero in a block that the table does not name).
 template <typename C, int D, bool PAGED>
 __device__ inline f32x4 v_at(const AttnArgs &a, const int32_t *table_row, int64_t seq_row0, int kvh, int tok, int d) {
     const char *p;
@@ -227,7 +251,7 @@ __device__ inline f32x4 v_at(const AttnArgs &a, const int32_t *table_row, int64_
     }
     const C *e = (const C *)p + d;
     if constexpr (sizeof(C) == 1) {
-        const uint2 x = bf16_of_fp8(*(const uint32_t *)e);
+        const uint2 x = bf16_of4<C>(*(const uint32_t *)e);
         return f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
                      __uint_as_float(x.y & 0xFFFF0000u)};
     } else {

@@ -31,7 +31,13 @@ constexpr float kLag = 8.f;
 // LDS: rows of 16-byte pieces; keys padded by one piece (the 16 rows of a piece
 // fall on different banks), values by four (the 8 rows x 64 bytes of a
 // fragment's transposed reads fall on every bank twice).
-template <int D> struct WideLds {
+//
+// Scales of the key tiles of which scores or weights are still to come, four runs of 16
+// keys each: (what scores are multiplied by, what weights are).
+template <bool SCALES> struct TileScales {};
+template <> struct TileScales<true> { float2 scales[4][4]; };
+
+template <typename C, int D> struct WideLds : TileScales<kScaleScores<C>> {
     static constexpr int KT = 64, PPR = D / 8, KS = PPR + 1, VS = PPR + 4;
     union {
         struct {
@@ -50,8 +56,9 @@ __device__ inline float half_max(float x) {
 }
 
 template <typename C, int D, bool PAGED>
-__device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, WideLds<D> &sm) {
-    using L = WideLds<D>;
+__device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, WideLds<C, D> &sm) {
+    using L = WideLds<C, D>;
+    constexpr bool SCORES = kScaleScores<C>;
     constexpr int KT = L::KT, PPR = L::PPR, RPL = 64 / PPR, LOADS = KT / (4 * RPL), KD = D / 16, MT32 = D / 32;
     constexpr int CB = 8 * sizeof(C), RB = D * sizeof(C);
 
@@ -65,15 +72,24 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     const uint32_t kvoff = ld.voff(lrow, a.kv.k_stride, lp * CB), vvoff = ld.voff(lrow, a.kv.v_stride, lp * CB);
     typename Loads::Place kplace, vplace;
     Raw<C> fk[LOADS], fv[LOADS];
+    // The tile's scales wait in LDS, four tiles' worth: written two turns before they are
+    // read, with a barrier in between.
+    auto place = [&](int t0) {
+        ld.place(a.kv, t0, &kplace);
+        if constexpr (SCORES) {
+            const int r = lane - (t0 - ld.base) / kRunTokens;
+            if (wave == 0 && (unsigned)r < 4u) sm.scales[(t0 - t.lo) / KT & 3][r] = make_float2(run_factor(a.c, ld.runs.ks), ld.runs.vs);
+        }
+    };
     // A turn's loads: keys of the tile at t0, values of the tile before it.
     auto loads = [&](int t0) {
         vplace = kplace;
         ld.load(fv, a.kv.v, vplace, a.kv.v_stride, vvoff, t0 - KT, KT);
-        ld.place(a.kv, t0, &kplace);
+        place(t0);
         ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t0, KT);
     };
     ld.begin(a.kv, t.lo);
-    ld.place(a.kv, t.lo, &kplace);
+    place(t.lo);
     ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t.lo, KT);
 
     const int row = t.row0 + 32 * wave + col;
@@ -93,13 +109,13 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
 
     auto store_k = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = Loads::piece(fk[i], kplace, i);
+        for (int i = 0; i < LOADS; ++i) sm.k[b][((4 * i + wave) * RPL + lrow) * L::KS + lp] = Loads::piece(fk[i], kplace, i, false);
     };
     auto store_v = [&](int b, bool mixed) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            uint4 v = Loads::piece(fv[i], vplace, i);
-            if (mixed && has_nonfinite<__bf16>(v)) {
+            uint4 v = Loads::piece(fv[i], vplace, i, true);
+            if (!SCORES && mixed && has_nonfinite<__bf16>(v)) {      // integer codes are finite
                 drop_nonfinite<__bf16>(v);
                 sm.dropped = 1;
             }
@@ -128,10 +144,21 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = seen > 8 * (i >> 2) + (i & 3) ? s[i] : -INFINITY;
         }
-        float top = fmaxf(s[0], s[1]);
+        float4 f = make_float4(a.c, 1.f, a.c, 1.f);      // of scores and weights of the half's two runs: elements 0 to 7, 8 to 15
+        if constexpr (SCORES) f = *(const float4 *)&sm.scales[(t0 - t.lo) / KT & 3][(t0 - t.lo) / 16 & 2];
+        float top = fmaxf(s[0], s[1]), top1 = fmaxf(s[8], s[9]);
 #pragma unroll
-        for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
-        top = half_max(top) * a.c;
+        for (int i = 2; i < 8; i += 2) {
+            top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
+            if constexpr (SCORES) top1 = fmaxf(fmaxf(top1, s[8 + i]), s[9 + i]);
+        }
+        if constexpr (SCORES) {
+            top = half_max(fmaxf(top * f.x, top1 * f.z));
+        } else {
+#pragma unroll
+            for (int i = 8; i < 16; i += 2) top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
+            top = half_max(top) * a.c;
+        }
         float shrink = 1.f;
         if (top > m + kLag) {
             shrink = __builtin_amdgcn_exp2f(m - top);
@@ -142,8 +169,9 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
         float e[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -mu));
+            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], i < 8 ? f.x : f.z, -mu));
             l += e[i];
+            if constexpr (SCORES) e[i] *= i < 8 ? f.y : f.w;
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -266,7 +294,7 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
 
 template <typename C, int D, bool PAGED>
 __global__ __launch_bounds__(kWideThreads, 2) void attn_wide_kernel(AttnArgs a) {
-    __shared__ WideLds<D> sm;
+    __shared__ WideLds<C, D> sm;
     RowTile t;
     if (prompt_tile_of<kPromptRows>(a, blockIdx.x, &t)) wide_run<C, D, PAGED>(a, t, sm);
 }

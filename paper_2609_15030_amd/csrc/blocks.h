@@ -423,26 +423,10 @@ struct KvWriteArgs {
     int32_t *err;
     float k_scale, v_scale;        // what a stored 8-bit 1 stands for
     int32_t n_seqs, kv_heads, n_blocks, bt_shift;
+    char *ks, *vs;                 // block-scaled cache: the layer's scales in block 0
 };
 
 constexpr int kWriteTokens = 4;    // tokens a workgroup writes, one for each wave
-
-// The sequence of row `tok`, by offsets cu [n + 1], one sequence a lane; its rows are
-// [*first, *end).  False for rows before the first sequence and behind the last.
-__device__ inline bool sequence_of(const int32_t *cu, int n, int tok, int *seq, int *first, int *end) {
-    const int lane = threadIdx.x & 63;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = min(i0 + lane, n - 1), c0 = cu[i], c1 = cu[i + 1];
-        const uint64_t past = __ballot(c1 > tok);
-        if (!past) continue;
-        const int at = __builtin_ctzll(past);
-        *seq = i0 + at;
-        *first = __builtin_amdgcn_readlane(c0, at);
-        *end = __builtin_amdgcn_readlane(c1, at);
-        return *first <= tok;
-    }
-    return false;
-}
 
 // Four values to e4m3: beyond the largest finite value they become it, NaN stays.
 __device__ inline uint32_t fp8_of4(const float *x) {

@@ -30,6 +30,14 @@ LA_ERR_WORKSPACE = 6
 LA_F32 = 0
 LA_BF16 = 1
 LA_FP8_E4M3 = 2
+LA_FP8_E4M3_BLOCK = 3
+LA_INT8_BLOCK = 4
+LA_ROPE_HALVES = 0
+LA_ROPE_PAIRS = 1
+LA_ROPE_UNSCALED = 0
+LA_ROPE_LINEAR = 1
+LA_ROPE_BASE = 2
+LA_ROPE_PARTS = 3
 LA_GDR_LITERAL = 0
 LA_GDR_DECAYED_DELTA = 1
 
@@ -39,7 +47,8 @@ EXPORTED = ("strict_prefix_boundary", "la_prefill_workspace_bytes", "la_prefill"
             "la_state_restore_paged",
             "la_state_save_host", "la_state_restore_host", "la_hybrid_boundary", "la_hybrid_restore",
             "la_attn_prefill", "la_attn_prefill_paged", "la_attn_prefill_workspace_bytes", "la_attn_decode",
-            "la_attn_decode_workspace_bytes", "la_kv_write", "la_blocks_copy", "la_blocks_fork", "la_blocks_extend",
+            "la_attn_decode_workspace_bytes", "la_kv_write", "la_kv_read", "la_rope_frequencies",
+            "la_rope_turns", "la_rope_apply", "la_blocks_copy", "la_blocks_fork", "la_blocks_extend",
             "la_blocks_free", "la_blocks_compact", "la_blocks_compact_workspace_bytes",
             "la_status_string", "la_last_error_message", "la_trace_set_events")
 
@@ -77,7 +86,28 @@ class LaKvLayer(ctypes.Structure):
                 ("k_offset", ctypes.c_int64), ("v_offset", ctypes.c_int64), ("block_tokens", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("block_table", ctypes.c_void_p),
-                ("max_blocks", ctypes.c_int64), ("err_count", ctypes.c_void_p)]
+                ("max_blocks", ctypes.c_int64), ("err_count", ctypes.c_void_p),
+                ("k_scales", ctypes.c_int64), ("v_scales", ctypes.c_int64)]
+
+
+class LaRopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class LaRopePlan(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("magnitude", ctypes.c_float), ("turns_dev", ctypes.c_void_p)]
+
+
+class LaRopeRows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("heads", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
+
+
+class LaRopePositions(ctypes.Structure):
+    _fields_ = [("positions_dev", ctypes.c_void_p), ("cu_seqlens_dev", ctypes.c_void_p), ("n_seqs", ctypes.c_int32),
+                ("kv_len_dev", ctypes.c_void_p)]
 
 
 class LaPrefixGroups(ctypes.Structure):
@@ -139,6 +169,11 @@ def _load() -> ctypes.CDLL:
         "la_attn_decode": ([AS, KL, P, P, I64, ctypes.POINTER(LaPrefixGroups), P, P, SZ, P], I32),
         "la_attn_decode_workspace_bytes": ([AS, I64, I64], SZ),
         "la_kv_write": ([KL, I32, P, I64, P, I64, P, I32, I64, P, P], I32),
+        "la_kv_read": ([KL, I32, P, I64, P, I64, P, I32, I64, P, P], I32),
+        "la_rope_frequencies": ([I32, ctypes.c_double, ctypes.POINTER(LaRopeScaling), P], I32),
+        "la_rope_turns": ([P, I32, P], I32),
+        "la_rope_apply": ([ctypes.POINTER(LaRopePlan), ctypes.POINTER(LaRopeRows), ctypes.POINTER(LaRopeRows), I64,
+                           ctypes.POINTER(LaRopePositions), I32, P], I32),
         "la_blocks_copy": ([BP, P, P, I64, P], I32),
         "la_blocks_fork": ([BP, P, P, P, I64, P], I32),
         "la_blocks_extend": ([BP, P, P, I64, P], I32),
@@ -457,6 +492,7 @@ def la_hybrid_restore(kv: LaKvBlocks, boundary_dev, boundary_host, state_pool, s
 # ---------------------------------------------------------------------------
 
 _DTYPES = {torch.bfloat16: LA_BF16, torch.float32: LA_F32, torch.float8_e4m3fn: LA_FP8_E4M3}
+_CODES = {torch.float8_e4m3fn: LA_FP8_E4M3_BLOCK, torch.int8: LA_INT8_BLOCK}      # with scales in their blocks
 _TORCH = {v: k for k, v in _DTYPES.items()}
 _I32 = torch.int32
 
@@ -505,10 +541,13 @@ def make_attn_shape(n_seqs, q_heads, kv_heads, head_dim, io_dtype=LA_BF16, scale
 
 def make_kv_layer(cache, block_table, block_tokens: int, kv_heads: int, head_dim: int, dtype, k_offset: int = 0,
                   v_offset: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0,
-                  err_count=None) -> LaKvLayer:
+                  err_count=None, k_scales: Optional[int] = None, v_scales: Optional[int] = None) -> LaKvLayer:
     """la_kv_layer over a byte cache [n_blocks, block_bytes] (uint8) and a device
     int32 block table [n_seqs, max_blocks].  dtype: torch.bfloat16, float32 or
-    float8_e4m3fn; v_offset None: right behind the keys."""
+    float8_e4m3fn; v_offset None: right behind the keys.
+
+    k_scales: the offset of the block's own key scales, fp32 [kv_heads], for codes
+    of dtype float8_e4m3fn or int8 (v_scales None: right behind them)."""
     if cache.dim() != 2 or cache.dtype != torch.uint8:
         raise ValueError("expected a uint8 cache [n_blocks, block_bytes]")
     if block_table.dim() != 2:
@@ -516,9 +555,18 @@ def make_kv_layer(cache, block_table, block_tokens: int, kv_heads: int, head_dim
     size = torch.empty(0, dtype=dtype).element_size()
     if v_offset is None:
         v_offset = k_offset + kv_heads * block_tokens * head_dim * size
+    if k_scales is None:
+        if v_scales is not None or dtype is torch.int8:
+            raise ValueError("codes with a scale for each block need k_scales")
+        code, k_scales, v_scales = _dtype_of(dtype), 0, 0
+    else:
+        code = _CODES.get(dtype)
+        if code is None:
+            raise ValueError(f"scales for each block go with float8_e4m3fn and int8 codes, not {dtype}")
+        v_scales = k_scales + 4 * kv_heads if v_scales is None else v_scales
     y = LaKvLayer(_dptr(cache), cache.shape[0], cache.shape[1], k_offset, v_offset, block_tokens, kv_heads, head_dim,
-                  _dtype_of(dtype), k_scale, v_scale, _ids(block_table, "block_table"), block_table.shape[1],
-                  _ids(err_count, "err_count"))
+                  code, k_scale, v_scale, _ids(block_table, "block_table"), block_table.shape[1],
+                  _ids(err_count, "err_count"), k_scales, v_scales)
     y._keep = (cache, block_table, err_count)       # the struct holds raw addresses only
     y._seqs = block_table.shape[0]
     return y
@@ -639,6 +687,99 @@ def la_kv_write(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: 
     (kp, ks), (vp, vs) = _rows(k, dt, kv), _rows(v, dt, kv)
     st = _lib.la_kv_write(ctypes.byref(layer), _dtype_of(dt), kp, ks, vp, vs, _ids(cu_dev, "cu_seqlens"), n_seqs, kv[0],
                           _ids(kv_len_dev, "kv_len"), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+def la_kv_read(layer: LaKvLayer, k, v, cu_dev, kv_len_dev, stream=None, check: bool = True) -> int:
+    """Cached rows of the sequences of cu_dev [n_seqs + 1] into k, v [T, kv_heads, d]."""
+    n_seqs, dt = cu_dev.numel() - 1, k.dtype
+    if layer._seqs < n_seqs or kv_len_dev.numel() < n_seqs:
+        raise ValueError("the block table or kv_len has fewer rows than the call sequences")
+    kv = (k.shape[0], layer.kv_heads, layer.head_dim)
+    (kp, ks), (vp, vs) = _rows(k, dt, kv), _rows(v, dt, kv)
+    st = _lib.la_kv_read(ctypes.byref(layer), _dtype_of(dt), kp, ks, vp, vs, _ids(cu_dev, "cu_seqlens"), n_seqs, kv[0],
+                         _ids(kv_len_dev, "kv_len"), _stream(stream))
+    if check:
+        _check(st)
+    return st
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+
+_SCALINGS = {"linear": LA_ROPE_LINEAR, "base": LA_ROPE_BASE, "parts": LA_ROPE_PARTS}
+_LAYOUTS = {"halves": LA_ROPE_HALVES, "pairs": LA_ROPE_PAIRS}
+
+
+def make_rope_scaling(kind: str, factor: float, original_len: float = 0.0, low: float = 0.0,
+                      high: float = 0.0) -> LaRopeScaling:
+    """kind: "linear", "base" or "parts" (with original_len, low and high)."""
+    if kind not in _SCALINGS:
+        raise ValueError(f"no scaling {kind!r}: one of {', '.join(_SCALINGS)}")
+    return LaRopeScaling(_SCALINGS[kind], factor, original_len, low, high)
+
+
+def la_rope_frequencies(rotary_dim: int, base: float, scaling: Optional[LaRopeScaling] = None) -> np.ndarray:
+    """Radians a token of each pair, fp64 [rotary_dim / 2]."""
+    freq = np.zeros(max(0, rotary_dim // 2), np.float64)
+    _check(_lib.la_rope_frequencies(int(rotary_dim), float(base), None if scaling is None else ctypes.byref(scaling),
+                                    _hptr(freq, np.float64)))
+    return freq
+
+
+def la_rope_turns(freq) -> np.ndarray:
+    """Frequencies as la_rope_apply reads them, uint64."""
+    freq = np.ascontiguousarray(freq, np.float64)
+    turns = np.zeros(freq.shape[0], np.uint64)
+    _check(_lib.la_rope_turns(_hptr(freq, np.float64), freq.shape[0], _hptr(turns, np.uint64)))
+    return turns
+
+
+def make_rope_plan(head_dim: int, rotary_dim: int, layout: str, io_dtype: int, turns, magnitude: float = 1.0) -> LaRopePlan:
+    """layout: "halves" or "pairs"; turns: device int64 [rotary_dim / 2] with the bits of la_rope_turns."""
+    if layout not in _LAYOUTS:
+        raise ValueError(f"no layout {layout!r}: one of {', '.join(_LAYOUTS)}")
+    if turns.dtype is not torch.int64 or turns.numel() != rotary_dim // 2:
+        raise ValueError("expected int64 turns, one for each pair")
+    p = LaRopePlan(head_dim, rotary_dim, _LAYOUTS[layout], io_dtype, magnitude, _dptr(turns))
+    p._keep = turns                                 # the struct holds raw addresses only
+    return p
+
+
+def la_rope_apply(plan: LaRopePlan, q, q_out, k=None, k_out=None, positions=None, cu_dev=None, kv_len_dev=None,
+                  transpose: bool = False, stream=None, check: bool = True) -> int:
+    """q, k [T, heads, head_dim] (either may be None) turned into q_out, k_out,
+    which may be q and k themselves.  positions: device int32 [T]; or cu_dev
+    [n_seqs + 1] and kv_len_dev [n_seqs], as la_kv_write takes them."""
+    dt, rows, T = _TORCH[plan.io_dtype], [], None
+    for x, y in ((q, q_out), (k, k_out)):
+        if (x is None) != (y is None):
+            raise ValueError("an input goes with an output")
+        if x is None:
+            rows.append(None)
+            continue
+        if x.dim() != 3 or (T is not None and x.shape[0] != T):
+            raise ValueError("expected q and k [T, heads, head_dim] of as many tokens")
+        T = x.shape[0]
+        shape = (T, x.shape[1], plan.head_dim)
+        (xp, xs), (yp, ys) = _rows(x, dt, shape), _rows(y, dt, shape)
+        rows.append(LaRopeRows(xp, yp, x.shape[1], xs, ys))
+    if (positions is None) == (cu_dev is None) or (cu_dev is None) != (kv_len_dev is None):
+        raise ValueError("expected positions, or cu_seqlens with kv_len")
+    n_seqs = 0
+    if positions is not None:
+        if T is not None and positions.numel() != T:
+            raise ValueError("expected a position for each token")
+    else:
+        n_seqs = cu_dev.numel() - 1
+        if kv_len_dev.numel() < n_seqs:
+            raise ValueError("kv_len has fewer entries than the call sequences")
+    at = LaRopePositions(_ids(positions, "positions"), _ids(cu_dev, "cu_seqlens"), n_seqs, _ids(kv_len_dev, "kv_len"))
+    a, b = (None if r is None else ctypes.byref(r) for r in rows)
+    st = _lib.la_rope_apply(ctypes.byref(plan), a, b, T or 0, ctypes.byref(at), int(transpose), _stream(stream))
     if check:
         _check(st)
     return st
