@@ -304,4 +304,20 @@ __device__ inline bool sequence_of(const int32_t *cu, int n, int tok, int *seq, 
     return false;
 }
 
+// The same, and the row's position, which is its place from the end of kv_len's keys: the
+// lengths are read beside the offsets, not after the sequence is known.
+__device__ inline bool position_of(const int32_t *cu, const int32_t *kv_len, int n, int tok, int *seq, int *pos) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = min(i0 + lane, n - 1), c0 = cu[i], c1 = cu[i + 1], len = kv_len[i];
+        const uint64_t past = __ballot(c1 > tok);
+        if (!past) continue;
+        const int at = __builtin_ctzll(past);
+        *seq = i0 + at;
+        *pos = __builtin_amdgcn_readlane(len, at) - (__builtin_amdgcn_readlane(c1, at) - tok);
+        return __builtin_amdgcn_readlane(c0, at) <= tok;
+    }
+    return false;
+}
+
 }  // namespace la

@@ -17,9 +17,11 @@ namespace la {
 // of a block that the table does not name are made zero on their way to LDS
 // (missing).  Everything but `voff` is uniform.
 template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvLoads {
+    static constexpr uint32_t kExponent = 0x7F800000;
+    static constexpr int STEP_TOKENS = 64 * kRunTokens;      // tokens of `runs`
     static constexpr int STEP = NW * RPL;        // rows from one run of a wave to the next
     static_assert(STEP % kRunTokens == 0 || kRunTokens % STEP == 0, "a wave's rows lie in one run of 16");
-    struct Scales { float k[LOADS], v[LOADS]; };
+    struct Scales { uint32_t scales[LOADS]; };   // exponents: of keys from bit 23 on, of values from bit 15
     struct None {};
     struct Place : std::conditional_t<kScaleCodes<C>, Scales, None> {
         int64_t at[LOADS];
@@ -30,36 +32,52 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
     int kvh, hi, wave;
     Runs runs;
     int base, next;                              // first token of `runs`; the lane's block id of the 1,024 tokens behind
-    float next_ks, next_vs;                      // their scales: loaded at the first tile after `next`, so that no tile waits for either
-    bool ahead;
+    // Block-scaled: ids one step of 1,024 further ahead, and the scales of those in `next`.
+    // All of it is loaded where `base` moves: a load in a branch of its own had the
+    // compiler wait for every load in flight on each tile (3 % of a large call).
+    int next2;
+    float next_ks, next_vs;
 
     __device__ inline void begin(const KvSource &s, int lo) {
         if constexpr (PAGED) {
-            base = lo & ~(64 * kRunTokens - 1);
+            base = lo & ~(STEP_TOKENS - 1);
             const int id = Runs::fetch(s, table_row, base, 0, hi);
-            next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
+            next = Runs::fetch(s, table_row, base, STEP_TOKENS, hi);
             runs.set(s, id, base, kvh, RB);
             if constexpr (kBlockScaled<C>) {
+                next2 = Runs::fetch(s, table_row, base, 2 * STEP_TOKENS, hi);
                 Runs::fetch_scales(s, id, base, 0, hi, kvh, &runs.ks, &runs.vs);
-                ahead = false;
+                Runs::fetch_scales(s, next, base, STEP_TOKENS, hi, kvh, &next_ks, &next_vs);
             }
+        }
+    }
+    // The exponents of a run's scales ride in the upper 17 bits of its offset (which needs
+    // 47 at most), so that no tile reads a lane more than the plain 8-bit cache does (eight
+    // reads a tile instead of sixteen).  The first tile goes ahead without them.
+    __device__ inline void join_scales(Place *first, int t0) {
+        if constexpr (kScaleCodes<C>) {
+            runs.at |= (int64_t)((__float_as_uint(runs.ks) & kExponent) | (__float_as_uint(runs.vs) & kExponent) >> 8) << 32;
+            const int r0 = ((t0 - base) + wave * RPL) / kRunTokens;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) first->scales[i] = (uint32_t)__builtin_amdgcn_readlane((int)(runs.at >> 32), r0 + i * STEP / kRunTokens);
         }
     }
     // The place of tile t0; tiles come in order.
     __device__ inline void place(const KvSource &s, int t0, Place *p) {
         if constexpr (PAGED) {
-            if (t0 - base >= 64 * kRunTokens) {
-                base += 64 * kRunTokens;
+            if (t0 - base >= STEP_TOKENS) {
+                base += STEP_TOKENS;
                 runs.set(s, next, base, kvh, RB);
-                next = Runs::fetch(s, table_row, base, 64 * kRunTokens, hi);
                 if constexpr (kBlockScaled<C>) {
                     runs.ks = next_ks;
                     runs.vs = next_vs;
-                    ahead = false;
+                    next = next2;
+                    Runs::fetch_scales(s, next, base, STEP_TOKENS, hi, kvh, &next_ks, &next_vs);
+                    next2 = Runs::fetch(s, table_row, base, 2 * STEP_TOKENS, hi);
+                    join_scales(p, t0);
+                } else {
+                    next = Runs::fetch(s, table_row, base, STEP_TOKENS, hi);
                 }
-            } else if (kBlockScaled<C> && !ahead && t0 > base) {
-                Runs::fetch_scales(s, next, base, 64 * kRunTokens, hi, kvh, &next_ks, &next_vs);
-                ahead = true;
             }
             const int r0 = ((t0 - base) + wave * RPL) / kRunTokens;
             p->missing = 0;
@@ -68,13 +86,13 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
                 for (int i = 0; i < LOADS; ++i) p->missing |= (uint32_t)!runs.named(r0 + i * STEP / kRunTokens) << i;
             }
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) p->at[i] = runs.run(r0 + i * STEP / kRunTokens) + i * STEP % kRunTokens * RB;
-            if constexpr (kScaleCodes<C>) {
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i) {
-                    p->k[i] = runs.k_scale(r0 + i * STEP / kRunTokens);
-                    p->v[i] = runs.v_scale(r0 + i * STEP / kRunTokens);
+            for (int i = 0; i < LOADS; ++i) {
+                int64_t at = runs.run(r0 + i * STEP / kRunTokens);
+                if constexpr (kScaleCodes<C>) {
+                    p->scales[i] = (uint32_t)(at >> 32);
+                    at &= 0x7FFFFFFFFFFF;
                 }
+                p->at[i] = at + i * STEP % kRunTokens * RB;
             }
         }
     }
@@ -97,7 +115,7 @@ template <typename C, bool PAGED, int NW, int RPL, int LOADS, int RB> struct KvL
     // Run i's piece of keys or values as it goes to LDS.
     __device__ static inline uint4 piece(const Raw<C> &f, const Place &p, int i, bool values = false) {
         if (PAGED && p.missing && (p.missing >> i & 1)) return make_uint4(0, 0, 0, 0);
-        if constexpr (kScaleCodes<C>) return piece_of<C>(f, values ? p.v[i] : p.k[i]);
+        if constexpr (kScaleCodes<C>) return piece_of<C>(f, __uint_as_float((values ? p.scales[i] << 8 : p.scales[i]) & kExponent));
         else return piece_of<C>(f);
     }
 };

@@ -74,8 +74,7 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     Raw<C> fk[LOADS], fv[LOADS];
     // The tile's scales wait in LDS, four tiles' worth: written two turns before they are
     // read, with a barrier in between.
-    auto place = [&](int t0) {
-        ld.place(a.kv, t0, &kplace);
+    auto keep_scales = [&](int t0) {
         if constexpr (SCORES) {
             const int r = lane - (t0 - ld.base) / kRunTokens;
             if (wave == 0 && (unsigned)r < 4u) sm.scales[(t0 - t.lo) / KT & 3][r] = make_float2(run_factor(a.c, ld.runs.ks), ld.runs.vs);
@@ -85,11 +84,12 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     auto loads = [&](int t0) {
         vplace = kplace;
         ld.load(fv, a.kv.v, vplace, a.kv.v_stride, vvoff, t0 - KT, KT);
-        place(t0);
+        ld.place(a.kv, t0, &kplace);
+        keep_scales(t0);
         ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t0, KT);
     };
     ld.begin(a.kv, t.lo);
-    place(t.lo);
+    ld.place(a.kv, t.lo, &kplace);
     ld.load(fk, a.kv.k, kplace, a.kv.k_stride, kvoff, t.lo, KT);
 
     const int row = t.row0 + 32 * wave + col;
@@ -207,6 +207,8 @@ __device__ __forceinline__ void wide_run(const AttnArgs &a, const RowTile &t, Wi
     // the weights of half 2 j and the scores of half 2 j + 1.
     f32x16 s0, s1;
     bf16x8 p0[2], p1[2];
+    if constexpr (PAGED) ld.join_scales(&kplace, t.lo);
+    keep_scales(t.lo);
     store_k(0);
     loads(t.lo + KT);
     __syncthreads();

@@ -128,12 +128,13 @@ __device__ inline uint32_t wave_most(uint32_t m) {
 // Sequence i's blocks have numbers from cu[i] / bt + 2 i on, so that a workgroup finds
 // its own without a sum over the sequences before it: n tokens lie in at most n / bt + 2
 // blocks.
-__device__ inline bool spot_of(const KvWriteArgs &a, int64_t w, int *seq, int *c0, int *c1, int64_t *nth) {
+__device__ inline bool spot_of(const KvWriteArgs &a, int64_t w, int *seq, int *c0, int *c1, int *len, int64_t *nth) {
     const int lane = threadIdx.x & 63;
     // no sequence before (w - n_tokens / bt) / 2 has this number
     const int64_t least = (w - (a.n_tokens >> a.bt_shift)) / 2 - 1;
     for (int i0 = (int)max((int64_t)0, least) & ~63; i0 < a.n_seqs; i0 += 64) {
         const int i = min(i0 + lane, a.n_seqs - 1);
+        const int n = a.kv_len[i];                 // beside the offsets, not after the sequence is known
         const int64_t b0 = max(a.cu[i], 0), b1 = min((int64_t)max(a.cu[i + 1], 0), a.n_tokens);
         const int64_t first = (b0 >> a.bt_shift) + 2 * (int64_t)i, end = (b1 >> a.bt_shift) + 2 * (int64_t)(i + 1);
         const uint64_t past = __ballot(end > w);
@@ -142,6 +143,7 @@ __device__ inline bool spot_of(const KvWriteArgs &a, int64_t w, int *seq, int *c
         *seq = i0 + l;
         *c0 = __builtin_amdgcn_readlane((int)b0, l);
         *c1 = __builtin_amdgcn_readlane((int)b1, l);
+        *len = __builtin_amdgcn_readlane(n, l);
         *nth = w - (((int64_t)__builtin_amdgcn_readlane((int)(first >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)first, l));
         return *nth >= 0 && *c1 > *c0;
     }
@@ -164,10 +166,10 @@ __global__ __launch_bounds__(256) void kv_write_codes_kernel(KvCodesArgs args) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t group = args.first_group + blockIdx.x, w = group / args.unit_groups;
     const int ug = (int)(group - w * args.unit_groups);
-    int seq, c0, c1;
+    int seq, c0, c1, keys;
     int64_t nth;
-    if (!spot_of(a, w, &seq, &c0, &c1, &nth)) return;
-    const int64_t len = a.kv_len[seq], p0 = len - (c1 - c0), j = (p0 >> a.bt_shift) + nth, base = j * (1 << a.bt_shift);
+    if (!spot_of(a, w, &seq, &c0, &c1, &keys, &nth)) return;
+    const int64_t len = keys, p0 = len - (c1 - c0), j = (p0 >> a.bt_shift) + nth, base = j * (1 << a.bt_shift);
     if (base >= len) return;
     const int id = j >= 0 && j < a.max_blocks ? a.table[seq * a.max_blocks + j] : -1;
     if ((uint32_t)id >= (uint32_t)a.n_blocks) {
@@ -264,16 +266,16 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvWriteArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t tok = a.first_token + (int64_t)blockIdx.x * kWriteTokens + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (tok >= a.n_tokens) return;
-    int seq, first, end;
-    if (!sequence_of(a.cu, a.n_seqs, (int)tok, &seq, &first, &end)) return;
-    const int64_t pos = (int64_t)a.kv_len[seq] - (end - tok), j = pos >> a.bt_shift;
+    int seq, pos;
+    if (!position_of(a.cu, a.kv_len, a.n_seqs, (int)tok, &seq, &pos)) return;
+    const int64_t j = pos >> a.bt_shift;
     int id = pos >= 0 && j < a.max_blocks ? a.table[seq * a.max_blocks + j] : -1;
     const bool named = (uint32_t)id < (uint32_t)a.n_blocks;
     if (!named) {
         if (lane == 0 && a.err) atomicAdd(a.err, 1);
         id = 0;
     }
-    const int slot = (int)pos & ((1 << a.bt_shift) - 1);
+    const int slot = pos & ((1 << a.bt_shift) - 1);
     constexpr int V = D / 8;
     const int pieces = a.kv_heads * V;
     const int64_t block = (int64_t)id * a.block_bytes;

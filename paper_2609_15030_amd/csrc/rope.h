@@ -120,16 +120,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         if (!PAIRS && turned) x2[i].load(px + half + d, n[i]);
     }
 
+    const uint64_t turns0 = a.turns[min(lane, half - 1)];          // in flight beside what the position takes
     int pos;
     if (a.positions) {
         pos = a.positions[tok];
     } else {
-        int seq, first, end;
-        if (!sequence_of(a.cu, a.n_seqs, (int)tok, &seq, &first, &end)) return;
-        pos = a.kv_len[seq] - (end - (int)tok);
+        int seq;
+        if (!position_of(a.cu, a.kv_len, a.n_seqs, (int)tok, &seq, &pos)) return;
     }
     for (int i = lane; i < half; i += 64) {
-        float2 t = cos_sin((uint32_t)((uint64_t)(int64_t)pos * a.turns[i] >> 32));
+        const uint64_t turns = i < 64 ? turns0 : a.turns[i];
+        float2 t = cos_sin((uint32_t)((uint64_t)(int64_t)pos * turns >> 32));
         t.x *= a.magnitude;
         t.y *= a.transpose ? -a.magnitude : a.magnitude;
         turn_sm[wave][i] = t;

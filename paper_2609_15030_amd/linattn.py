@@ -754,35 +754,46 @@ def la_rope_apply(plan: LaRopePlan, q, q_out, k=None, k_out=None, positions=None
     """q, k [T, heads, head_dim] (either may be None) turned into q_out, k_out,
     which may be q and k themselves.  positions: device int32 [T]; or cu_dev
     [n_seqs + 1] and kv_len_dev [n_seqs], as la_kv_write takes them."""
-    dt, rows, T = _TORCH[plan.io_dtype], [], None
-    for x, y in ((q, q_out), (k, k_out)):
-        if (x is None) != (y is None):
-            raise ValueError("an input goes with an output")
-        if x is None:
-            rows.append(None)
-            continue
-        if x.dim() != 3 or (T is not None and x.shape[0] != T):
-            raise ValueError("expected q and k [T, heads, head_dim] of as many tokens")
-        T = x.shape[0]
-        shape = (T, x.shape[1], plan.head_dim)
-        (xp, xs), (yp, ys) = _rows(x, dt, shape), _rows(y, dt, shape)
-        rows.append(LaRopeRows(xp, yp, x.shape[1], xs, ys))
-    if (positions is None) == (cu_dev is None) or (cu_dev is None) != (kv_len_dev is None):
-        raise ValueError("expected positions, or cu_seqlens with kv_len")
-    n_seqs = 0
+    dt, dim, T = _TORCH[plan.io_dtype], plan.head_dim, 0
+    a = b = None
+    if q is not None:
+        a, T = _rope_rows(q, q_out, dt, dim)
+    if k is not None:
+        b, n = _rope_rows(k, k_out, dt, dim)
+        if q is not None and n != T:
+            raise ValueError("expected q and k of as many tokens")
+        T = n
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output goes with an input")
     if positions is not None:
-        if T is not None and positions.numel() != T:
+        if cu_dev is not None or kv_len_dev is not None:
+            raise ValueError("expected positions, or cu_seqlens with kv_len")
+        if positions.numel() != T and (q is not None or k is not None):
             raise ValueError("expected a position for each token")
+        at = LaRopePositions(_ids(positions, "positions"), None, 0, None)
     else:
+        if cu_dev is None or kv_len_dev is None:
+            raise ValueError("expected positions, or cu_seqlens with kv_len")
         n_seqs = cu_dev.numel() - 1
         if kv_len_dev.numel() < n_seqs:
             raise ValueError("kv_len has fewer entries than the call sequences")
-    at = LaRopePositions(_ids(positions, "positions"), _ids(cu_dev, "cu_seqlens"), n_seqs, _ids(kv_len_dev, "kv_len"))
-    a, b = (None if r is None else ctypes.byref(r) for r in rows)
-    st = _lib.la_rope_apply(ctypes.byref(plan), a, b, T or 0, ctypes.byref(at), int(transpose), _stream(stream))
+        at = LaRopePositions(None, _ids(cu_dev, "cu_seqlens"), n_seqs, _ids(kv_len_dev, "kv_len"))
+    st = _lib.la_rope_apply(plan, a, b, T, at, transpose, _stream(stream))       # ctypes passes structs by address
     if check:
         _check(st)
     return st
+
+
+def _rope_rows(x, y, dt, dim: int):
+    """(la_rope_rows, tokens) of x and the tensor it is turned into."""
+    if y is None or x.dim() != 3:
+        raise ValueError("expected [T, heads, head_dim], and an output with it")
+    T, heads, _ = shape = x.shape
+    if shape[2] != dim:
+        raise ValueError(f"expected heads of {dim}, got {shape[2]}")
+    xp, xs = _rows(x, dt, shape)
+    yp, ys = (xp, xs) if y is x else _rows(y, dt, shape)
+    return LaRopeRows(xp, yp, heads, xs, ys), T
 
 
 def _same_count(*lists):
