@@ -17,10 +17,15 @@ with it, and several samples of the second one:
    is retired (la_blocks_free) and the blocks close up (la_blocks_compact)
    under the running samples.
 
+Queries and keys take their rotary positions before they are used
+(la_rope_apply, in place on the projection), and the blocks hold bf16, or 8-bit
+codes with a scale for each block and key head, which forks and compaction carry
+along as the bytes they are.
+
 Projections and sampling are left out: what they would give is drawn at
 random, keyed by the position, so that tokens two requests share are the same.
 
-    python examples/hybrid_request.py
+    python examples/hybrid_request.py [bf16 | e4m3 | int8]
 """
 from __future__ import annotations
 
@@ -50,6 +55,8 @@ class Sizes:
     second: int = 3328
     samples: int = 4
     steps: int = 16
+    rotary: int = 0                # dims of a head that take rotary positions (0: they are left out)
+    cache: str = "bf16"            # or "e4m3", "int8": codes with scales in their blocks
 
 
 @dataclasses.dataclass
@@ -87,7 +94,11 @@ class HybridCache:
     def __init__(self, s: Sizes, n_rows: int, max_tokens: int):
         self.s = s
         max_blocks = -(-max_tokens // s.block_tokens)
-        self.block_bytes = 2 * s.kv_heads * s.block_tokens * s.head_dim * 2
+        self.dtype = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[s.cache]
+        codes = 2 * s.kv_heads * s.block_tokens * s.head_dim
+        self.scales = None if s.cache == "bf16" else codes               # right behind keys and values
+        self.block_bytes = 2 * codes if s.cache == "bf16" else codes + -(-8 * s.kv_heads // 16) * 16
+        self.rope = api.Rope(s.head_dim, s.rotary) if s.rotary else None
         self.blocks = api.BlockPool.new(n_rows * max_blocks, self.block_bytes, s.block_tokens, n_rows, max_blocks)
         rows = n_rows * (max_tokens // s.interval) * s.heads
         self.states = torch.zeros((rows, s.head_dim * s.head_dim), device="cuda")
@@ -96,19 +107,23 @@ class HybridCache:
         """The attention layer's cache as sequences [row, row + n) see it."""
         s = self.s
         return la.make_kv_layer(self.blocks.cache, self.blocks.table[row:row + n], s.block_tokens, s.kv_heads,
-                                s.head_dim, torch.bfloat16, err_count=self.blocks.err_count)
+                                s.head_dim, self.dtype, err_count=self.blocks.err_count, k_scales=self.scales)
 
-    def qkv(self, t: torch.Tensor):
+    def qkv(self, t: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor):
+        """Queries and keys of a projection at their positions, and its values: slices of one tensor."""
         hq, hk = self.s.q_heads, self.s.kv_heads
+        if self.rope:
+            t = t.clone()                                                # the projection is drawn once for all tests
+            self.rope.apply(t[:, :hq], t[:, hq:hq + hk], cu_seqlens=cu, kv_len=kv_len)
         return t[:, :hq], t[:, hq:hq + hk], t[:, hq + hk:]
 
     def prompt(self, row: int, tokens: Tokens):
         """A cold prompt: (attention, recurrent result, its states' pages [checkpoints, heads])."""
         s, n = self.s, tokens.qkv.shape[0]
-        q, k, v = self.qkv(tokens.qkv)
-        attn = api.AttnPrefill(s.q_heads, s.kv_heads, s.head_dim, [n])
-        self.blocks.extend(_i32(row), _i32(n))
-        la.la_kv_write(self.layer(row), k, v, attn.cu_dev, _i32(n))
+        attn, kv_len = api.AttnPrefill(s.q_heads, s.kv_heads, s.head_dim, [n]), _i32(n)
+        q, k, v = self.qkv(tokens.qkv, attn.cu_dev, kv_len)
+        self.blocks.extend(_i32(row), kv_len)
+        la.la_kv_write(self.layer(row), k, v, attn.cu_dev, kv_len)
         rec = api.Prefill(api.to_device(tokens.rec), s.interval, emit_ckpt=False)
         pages = torch.arange(rec.n_ckpt_rows * s.heads, dtype=torch.int32, device="cuda")
         return attn.run(q, k, v), rec.run_paged(self.states, ckpt_page_ids=pages), pages.view(-1, s.heads)
@@ -117,8 +132,8 @@ class HybridCache:
         """A prompt whose first `boundary` tokens the parent row's cache holds: results from there on."""
         s, n = self.s, tokens.qkv.shape[0]
         new = tokens.part(boundary, n)
-        q, k, v = self.qkv(new.qkv)
         attn = api.AttnPrefill(s.q_heads, s.kv_heads, s.head_dim, [n - boundary], [n])
+        q, k, v = self.qkv(new.qkv, attn.cu_dev, attn.kv_dev)
         self.blocks.fork(_i32(parent), _i32(row), _i32(boundary))
         self.blocks.extend(_i32(row), _i32(n))
         la.la_kv_write(self.layer(row), k, v, attn.cu_dev, attn.kv_dev)
@@ -145,8 +160,8 @@ class HybridCache:
             if i == len(steps) // 2:
                 self.blocks.free(_i32(retire_row))
                 self.blocks.compact()
-            q, k, v = self.qkv(tokens.qkv)
             kv_len += 1
+            q, k, v = self.qkv(tokens.qkv, cu, kv_len)
             self.blocks.extend(rows, kv_len)
             la.la_kv_write(layer, k, v, cu, kv_len)
             outs.append(attn.run(layer, q, kv_len, shared).clone())
@@ -176,12 +191,13 @@ def serve(s: Sizes) -> dict:
 
 
 def main():
-    s = Sizes()
+    s = Sizes(rotary=128, cache=sys.argv[1] if len(sys.argv) > 1 else "bf16")
     r = serve(s)
     print(f"first prompt: {s.prompt} tokens, cold")
     print(f"second prompt: {s.second} tokens, {s.shared} of them shared; resumed at {r['boundary']}, "
           f"{s.second - r['boundary']} computed")
     print(f"{s.samples} samples of it: {s.steps} tokens each, {s.second // s.block_tokens} blocks shared")
+    print(f"cache in {s.cache}, {s.rotary} dims of a head turned by their positions")
     print(f"blocks in use {r['blocks'] - r['free']} of {r['blocks']}, errors {r['errors']}")
 
 
