@@ -352,28 +352,47 @@ la_status launch_kv_write(int d, la::KvWriteArgs &a, hipStream_t st) {
     return LA_OK;
 }
 
-// Pieces of 8 values a lane holds of a unit, and waves that share one.
-template <typename C, int D>
-la_status launch_kv_codes(la::KvCodesArgs &a, hipStream_t st) {
-    const int pieces = D / 8 << a.w.bt_shift;                  // of a unit
-    const bool small = pieces <= 4 * 64;
-    a.team_shift = pieces <= 16 * 64 ? 0 : pieces <= 32 * 64 ? 1 : 2;
-    a.unit_groups = (int32_t)up(2 * (int64_t)a.w.kv_heads << a.team_shift, 4);
+// P: pieces of 8 values a lane holds of a unit.
+template <typename C, int D, int P>
+la_status launch_kv_codes_of(la::KvCodesArgs &a, int waves, hipStream_t st) {
+    a.team_shift = shift_of(waves);
+    a.unit_groups = (int32_t)up(2 * (int64_t)a.w.kv_heads * waves, 4);
     const int64_t groups = ((a.w.n_tokens >> a.w.bt_shift) + 2 * (int64_t)a.w.n_seqs) * a.unit_groups, step = max_grid(256);
     for (a.first_group = 0; a.first_group < groups; a.first_group += step) {
         const dim3 grid((unsigned)std::min(groups - a.first_group, step));
-        if (small) hipLaunchKernelGGL((la::kv_write_codes_kernel<C, D, 4>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((la::kv_write_codes_kernel<C, D, 16>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((la::kv_write_codes_kernel<C, D, P>), grid, dim3(256), 0, st, a);
         if (la_status e = hip_check("cache write launch")) return e;
     }
     return LA_OK;
 }
 
+// One wave a unit while its registers hold it, four beyond (39,934 tokens x 8 heads: blocks
+// of 128 x 128 values in four waves of 8 pieces 53 us, in two of 16 56; blocks of 64 x 128
+// in one wave of 16 pieces 53, in two of 8 54).
+template <typename C, int D>
+la_status launch_kv_codes(la::KvCodesArgs &a, hipStream_t st) {
+    const int pieces = (D / 8 << a.w.bt_shift) / 64;           // of a unit for each lane of a wave
+    if constexpr (D == 64) {
+        if (pieces == 2) return launch_kv_codes_of<C, D, 2>(a, 1, st);
+    }
+    switch (pieces) {
+    case 4: return launch_kv_codes_of<C, D, 4>(a, 1, st);
+    case 8: return launch_kv_codes_of<C, D, 8>(a, 1, st);
+    case 16: return launch_kv_codes_of<C, D, 16>(a, 1, st);
+    case 32: return launch_kv_codes_of<C, D, 8>(a, 4, st);
+    default: return launch_kv_codes_of<C, D, 16>(a, 4, st);
+    }
+}
+
 template <typename T, typename C>
-la_status launch_kv_read(int d, la::KvWriteArgs &a, hipStream_t st) {
-    constexpr int64_t STEP = max_grid(256) * la::kWriteTokens;
-    for (a.first_token = 0; a.first_token < a.n_tokens; a.first_token += STEP) {
-        const dim3 grid((unsigned)up(std::min(a.n_tokens - a.first_token, STEP), la::kWriteTokens));
+la_status launch_kv_read(int d, const la::KvWriteArgs &w, hipStream_t st) {
+    la::KvReadArgs a{};
+    a.w = w;
+    a.lanes = (int32_t)std::min<int64_t>(64, up(2 * (int64_t)w.kv_heads * d * (int64_t)sizeof(T) / 16, 4));
+    a.by_lanes = la::FastDiv::by((uint32_t)a.lanes);
+    const int64_t tokens = 64 / a.lanes * la::kWriteTokens, step = max_grid(256) * tokens;    // of a workgroup, of a launch
+    for (a.w.first_token = 0; a.w.first_token < w.n_tokens; a.w.first_token += step) {
+        const dim3 grid((unsigned)up(std::min(w.n_tokens - a.w.first_token, step), tokens));
         if (d == 64) hipLaunchKernelGGL((la::kv_read_kernel<T, C, 64>), grid, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((la::kv_read_kernel<T, C, 128>), grid, dim3(256), 0, st, a);
         if (la_status e = hip_check("cache read launch")) return e;

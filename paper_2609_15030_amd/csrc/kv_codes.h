@@ -121,9 +121,9 @@ __device__ inline uint32_t wave_most(uint32_t m) {
     return x;
 }
 
-// Workgroups of four waves take units of one block that the call writes into; 1, 2 or 4
-// waves a unit, each with up to P pieces of 8 values a lane in registers, so that values
-// are read once and a block's scale is known before any of its codes is formed.
+// Workgroups of four waves take units of one block that the call writes into, one or four
+// waves a unit, each with P pieces of 8 values a lane in registers, so that values are
+// read once and a block's scale is known before any of its codes is formed.
 //
 // Sequence i's blocks have numbers from cu[i] / bt + 2 i on, so that a workgroup finds
 // its own without a sum over the sequences before it: n tokens lie in at most n / bt + 2
@@ -204,7 +204,8 @@ __global__ __launch_bounds__(256) void kv_write_codes_kernel(KvCodesArgs args) {
 #pragma unroll
     for (int i = 0; i < P; ++i) m = most_of(m, raw[i]);
     uint32_t most = wave_most(m);
-    // the waves of a unit agree on its magnitude; its old scale is read by one, before another may have written the new
+    // The waves of a unit agree on its magnitude; its old scale is read by one, before
+    // another may have written the new.
     auto agree = [&]() {
         if (team == 1) return;
         __syncthreads();
@@ -217,19 +218,16 @@ __global__ __launch_bounds__(256) void kv_write_codes_kernel(KvCodesArgs args) {
         old = old_sm[wave - tw];
     };
     agree();
-    const bool odd = __builtin_amdgcn_readfirstlane((int)(most > kLargestBf16));
+    const bool odd = __builtin_amdgcn_readfirstlane((int)(most > kLargestBf16));      // of a unit: not the same for the workgroup
     bool nan = false;
-    if (odd) {                                                 // uniform over the team, not over the workgroup
+    if (odd) {
         nan = most > 0x7F80u;
         m = 0;
 #pragma unroll
         for (int i = 0; i < P; ++i) m = most_finite_of(m, raw[i]);
         most = wave_most(m);
     }
-    if (team > 1) {
-        // a second round for all, since the barrier is the workgroup's
-        agree();
-    }
+    agree();                                                   // once more for all, since its barrier is the workgroup's
     float s = scale_of<C>(__uint_as_float(most << 16));
     if (a0 > 0) s = fmaxf(s, old);
     const float r = 1.f / s;
@@ -260,51 +258,92 @@ __global__ __launch_bounds__(256) void kv_write_codes_kernel(KvCodesArgs args) {
 
 // --- cached rows back out ----------------------------------------------------
 
-// A wave reads one token, as kv_write_kernel writes one: T of a row from C.
+struct KvReadArgs {
+    KvWriteArgs w;
+    int32_t lanes;                 // of a token, four pieces each (64: a wave takes one token, 256 pieces a turn)
+    FastDiv by_lanes;
+};
+
+// A wave takes as many tokens as fill it, four 16-byte pieces of the result a lane: with
+// one token a wave, few or short heads left most lanes without work (8 heads of 64: 1.3
+// times the time that a copy takes).  Sequences are found once, for the wave's first
+// token; a lane goes on from there to its own.
 template <typename T, typename C, int D>
-__global__ __launch_bounds__(256) void kv_read_kernel(KvWriteArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t tok = a.first_token + (int64_t)blockIdx.x * kWriteTokens + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (tok >= a.n_tokens) return;
-    int seq, pos;
-    if (!position_of(a.cu, a.kv_len, a.n_seqs, (int)tok, &seq, &pos)) return;
+__global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs args) {
+    const KvWriteArgs &a = args.w;
+    constexpr int N = 16 / sizeof(T), V = D / N, R = 4;        // values of a piece, pieces of a row, pieces of a lane
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = args.by_lanes(lane), per_wave = args.by_lanes(64);
+    const int64_t first = a.first_token + ((int64_t)blockIdx.x * kWriteTokens + wave) * per_wave, tok = first + group;
+    if (first >= a.n_tokens) return;
+    int seq = -1, end = 0;
+    for (int i0 = 0; i0 < a.n_seqs && seq < 0; i0 += 64) {
+        const int c1 = a.cu[min(i0 + lane, a.n_seqs - 1) + 1];
+        const uint64_t past = __ballot(c1 > first);
+        if (!past) continue;
+        const int at = __builtin_ctzll(past);
+        seq = i0 + at;
+        end = __builtin_amdgcn_readlane(c1, at);
+    }
+    if (seq < 0) return;
+    while (tok >= end) {
+        if (++seq >= a.n_seqs) return;
+        end = a.cu[seq + 1];
+    }
+    if (group >= per_wave || tok >= a.n_tokens || tok < a.cu[0]) return;
+    const int pos = a.kv_len[seq] - (end - (int)tok);
     const int64_t j = pos >> a.bt_shift;
     int id = pos >= 0 && j < a.max_blocks ? a.table[seq * a.max_blocks + j] : -1;
     const bool named = (uint32_t)id < (uint32_t)a.n_blocks;
+    const int l = lane - group * args.lanes, pieces = 2 * a.kv_heads * V;
     if (!named) {
-        if (lane == 0 && a.err) atomicAdd(a.err, 1);
+        if (l == 0 && a.err) atomicAdd(a.err, 1);
         id = 0;
     }
     const int slot = pos & ((1 << a.bt_shift) - 1);
-    constexpr int V = D / 8;
-    const int pieces = a.kv_heads * V;
     const int64_t block = (int64_t)id * a.block_bytes;
-    for (int e = lane; e < 2 * pieces; e += 64) {
-        const bool is_v = e >= pieces;
-        const int x = is_v ? e - pieces : e, h = x / V, p = x % V;
-        const char *src = (is_v ? a.cv : a.ck) + block + (((int64_t)h << a.bt_shift) + slot) * (int64_t)(D * sizeof(C)) + p * (int)(8 * sizeof(C));
-        T *dst = (is_v ? (T *)a.v : (T *)a.k) + tok * (is_v ? a.v_stride : a.k_stride) + h * D + p * 8;
-        f32x4 lo, hi;
-        if constexpr (sizeof(C) == 4) {
-            lo = *(const f32x4 *)src;
-            hi = *(const f32x4 *)(src + 16);
-        } else {
-            const uint4 b = piece_of<C>(*(const Raw<C> *)src);      // exact in bf16
-            auto pair = [](uint32_t x, uint32_t y) {
-                return f32x4{__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u), __uint_as_float(y << 16), __uint_as_float(y & 0xFFFF0000u)};
-            };
-            float s = 1.f;
-            if constexpr (kBlockScaled<C>) s = *((const float *)((is_v ? a.vs : a.ks) + block) + h);
-            else if constexpr (sizeof(C) == 1) s = is_v ? a.v_scale : a.k_scale;
-            lo = pair(b.x, b.y) * s;
-            hi = pair(b.z, b.w) * s;
+    typedef typename std::conditional<N * sizeof(C) == 16, uint4, typename std::conditional<N * sizeof(C) == 8, uint2, uint32_t>::type>::type Raw;
+    for (int e0 = l; e0 < pieces; e0 += R * args.lanes) {
+        Raw raw[R];
+        float s[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int e = min(e0 + i * args.lanes, pieces - 1);
+            const bool is_v = e >= a.kv_heads * V;
+            const int x = is_v ? e - a.kv_heads * V : e, h = x / V, p = x % V;
+            raw[i] = *(const Raw *)((is_v ? a.cv : a.ck) + block + (((int64_t)h << a.bt_shift) + slot) * (int64_t)(D * sizeof(C)) +
+                                    p * (int)(N * sizeof(C)));
+            s[i] = 1.f;
+            if constexpr (kBlockScaled<C>) s[i] = *((const float *)((is_v ? a.vs : a.ks) + block) + h);
+            else if constexpr (sizeof(C) == 1) s[i] = is_v ? a.v_scale : a.k_scale;
         }
-        if (!named) lo = hi = zero4();
-        if constexpr (sizeof(T) == 2) {
-            *(bf16x8 *)dst = pack8(lo, hi);
-        } else {
-            store4(dst, lo);
-            store4(dst + 4, hi);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int e = e0 + i * args.lanes;
+            if (e >= pieces) break;
+            const bool is_v = e >= a.kv_heads * V;
+            T *dst = (is_v ? (T *)a.v : (T *)a.k) + tok * (is_v ? a.v_stride : a.k_stride) + (is_v ? e - a.kv_heads * V : e) * N;
+            if constexpr (sizeof(C) == sizeof(T)) {                 // as it stands
+                *(uint4 *)dst = named ? raw[i] : make_uint4(0, 0, 0, 0);
+                continue;
+            }
+            const uint32_t *w = (const uint32_t *)&raw[i];
+            float f[N];
+#pragma unroll
+            for (int v = 0; v < N; v += 4) {
+                uint2 b{};                                          // four values in bf16, exact
+                if constexpr (sizeof(C) == 1) b = bf16_of4<C>(w[v / 4]);
+                else if constexpr (sizeof(C) == 2) b = make_uint2(w[v / 2], w[v / 2 + 1]);
+                f[v] = __uint_as_float(b.x << 16) * s[i];
+                f[v + 1] = __uint_as_float(b.x & 0xFFFF0000u) * s[i];
+                f[v + 2] = __uint_as_float(b.y << 16) * s[i];
+                f[v + 3] = __uint_as_float(b.y & 0xFFFF0000u) * s[i];
+            }
+#pragma unroll
+            for (int v = 0; v < N; ++v)
+                if (!named) f[v] = 0.f;
+            if constexpr (sizeof(T) == 2) *(bf16x8 *)dst = pack8(f32x4{f[0], f[1], f[2], f[3]}, f32x4{f[4], f[5], f[6], f[7]});
+            else store4(dst, f32x4{f[0], f[1], f[2], f[3]});
         }
     }
 }

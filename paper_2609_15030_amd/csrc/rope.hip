@@ -29,17 +29,22 @@ la_status check_rows(const la_rope_plan *p, const la_rope_rows *r, const char *w
     return LA_OK;
 }
 
-template <typename T>
-la_status launch(la::RopeArgs &a, bool pairs, hipStream_t st) {
-    constexpr int64_t STEP = 0xffffffffll / 256 * la::kRopeTokens;
-    const unsigned splits = (unsigned)((a.items + a.share - 1) / a.share);
-    for (a.first_token = 0; a.first_token < a.n_tokens; a.first_token += STEP) {
-        const dim3 grid((unsigned)((std::min(a.n_tokens - a.first_token, STEP) + la::kRopeTokens - 1) / la::kRopeTokens), splits);
-        if (pairs) hipLaunchKernelGGL((la::rope_kernel<T, true>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((la::rope_kernel<T, false>), grid, dim3(256), 0, st, a);
+template <typename T, bool PAIRS, bool SHORT>
+la_status launch_of(la::RopeArgs &a, hipStream_t st) {
+    constexpr int64_t SET = 8 * la::kRopeTokens;                   // tokens of eight workgroups
+    const int64_t step = 0x7fffffffll / (256 * 8) / a.splits * SET;            // of a launch
+    for (a.first_token = 0; a.first_token < a.n_tokens; a.first_token += step) {
+        const int64_t sets = (std::min(a.n_tokens - a.first_token, step) + SET - 1) / SET;
+        hipLaunchKernelGGL((la::rope_kernel<T, PAIRS, SHORT>), dim3((unsigned)(8 * sets * a.splits)), dim3(256), 0, st, a);
         if (la_status e = hip_check("rotary positions launch")) return e;
     }
     return LA_OK;
+}
+
+template <typename T>
+la_status launch(la::RopeArgs &a, bool pairs, hipStream_t st) {
+    if ((pairs ? a.rotary : a.rotary / 2) < la::Span<T>::N) return pairs ? launch_of<T, true, true>(a, st) : launch_of<T, false, true>(a, st);
+    return pairs ? launch_of<T, true, false>(a, st) : launch_of<T, false, false>(a, st);
 }
 
 }  // namespace
@@ -122,10 +127,11 @@ la_status la_rope_apply(const la_rope_plan *plan, const la_rope_rows *q, const l
     a.by_pieces = la::FastDiv::by((uint32_t)a.pieces);
     const int64_t items = ((int64_t)a.q.heads + a.k.heads) * a.pieces;
     a.items = (int32_t)items;                                  // rows of at most 2^24 values
-    const int32_t splits = (int32_t)((items + 64 * la::kRopeItems - 1) / (64 * la::kRopeItems));
-    a.share = (int32_t)((items + splits - 1) / splits + 63) & ~63;
+    a.splits = (int32_t)((items + 64 * la::kRopeItems - 1) / (64 * la::kRopeItems));
+    a.share = (int32_t)((items + a.splits - 1) / a.splits + 63) & ~63;
     a.magnitude = plan->magnitude;
     a.transpose = transpose != 0;
+    a.whole = (pairs ? r : r / 2) % n == 0;
     (void)hipGetLastError();
     return plan->io_dtype == LA_F32 ? launch<float>(a, pairs, (hipStream_t)stream) : launch<__bf16>(a, pairs, (hipStream_t)stream);
 }
