@@ -446,7 +446,9 @@ la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const i
  * infinity or NaN).  Values are summed before the division: beyond 2^120 / keys
  * the sums may overflow.  Scores, maxima and sums are fp32 (a token with a score past
  * fp32's range has NaN); with bf16 inputs the
- * weights p_j are rounded to bf16 for the product with v.  The same call
+ * weights p_j are rounded to bf16 for the product with v (times the value scale, where
+ * int8 codes have one for each block).  Keys and values of an 8-bit cache are what its
+ * codes stand for: k_scale or the block's scale times the code.  The same call
  * gives the same bits.  A single token's result does not depend on the other
  * sequences of its call (its group's prefix apart); a prompt's keys are summed
  * in parts where the whole call has few rows, so its last bits may differ
@@ -468,7 +470,8 @@ typedef struct la_attn_shape {
 /* One attention layer's keys and values in the cache.  Block b begins at cache
  * + b * block_bytes; at k_offset in it lie this layer's keys, at v_offset its
  * values, each [kv_heads, block_tokens, head_dim]; other layers share the
- * block.  Token x of sequence i is in slot x mod block_tokens of block
+ * block.  With a type of codes, this layer's scales lie in the block too: la_kv_write
+ * works them out, and whatever copies or moves blocks takes them along.  Token x of sequence i is in slot x mod block_tokens of block
  * block_table[i][x / block_tokens].  An entry outside [0, n_blocks) where a
  * key is visible or written counts in err_count (at least once; device
  * int32, may be NULL), reads as zero keys and values and is not written. */

@@ -14,6 +14,11 @@
 // shrinking, and follow it when it grows: code s_old / s, to nearest even.  With 8 bits
 // in s and in a bf16 value (15 in code s_old), a quotient is a tie or at least 2^-17 of
 // it away from one, so that one division, whoever does it, has one answer.
+//
+// Both kernels are bound by memory once they are large: 47,248 tokens x 8 heads x 128 as
+// e4m3 59.7 us (290 MB, 4.9 TB/s), 32,768 x 4 x 128 into int8 blocks of 64 21.2 (4.7);
+// 77,472 x 8 x 128 int8 back in bf16 94.9 (5.0).  Small calls are a chain of loads:
+// lengths, table, scale (64 tokens 4.5 us).
 #pragma once
 #include "blocks.h"
 

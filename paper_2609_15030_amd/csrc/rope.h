@@ -15,6 +15,10 @@
 // (i, i + r / 2)), at any alignment.  Where they do not divide a run of values, its last
 // piece reaches back over what is before it and stores only what is its own (in place it may
 // so read what another lane has turned already, and drops what it makes of it).
+//
+// Bound by memory: 32,768 tokens x 20 heads x 128 in bf16 66.2 us (335 MB, 5.1 TB/s).
+// Small calls are bound by what a position takes: lengths, angle, product (64 tokens 4.5
+// us).  Four to six pieces a lane were as fast or up to 8 % slower.
 #pragma once
 #include "attn_common.h"
 
