@@ -572,7 +572,8 @@ size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv
  * code * old / s, rounded to nearest even; a block's scale that no write can
  * have left counts as 2^-100.  Values beyond +-2^127 (infinities too) are
  * written as +-2^127.  NaN: e4m3 holds it; int8, which cannot, holds 0 and
- * counts in err_count.  A block is written for one sequence at a time.
+ * counts in err_count.  No call may write into one block through two entries
+ * of its tables.
  */
 la_status la_kv_write(const la_kv_layer *layer, int32_t io_dtype, const void *k, int64_t k_stride,
                       const void *v, int64_t v_stride, const int32_t *cu_seqlens_dev, int32_t n_seqs,

@@ -239,6 +239,8 @@ class Rope:
         """Turns q and k [T, heads, head_dim] at positions int32 [T], or at those
         of the sequences of cu_seqlens and kv_len (la_kv_write's); in place where no
         output is given.  transpose: the gradient.  Returns the outputs."""
+        if q is None and k is None:
+            raise ValueError("expected q, k or both")
         q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
         dtype = (k if q is None else q).dtype
         plan = self._plans.get(dtype)

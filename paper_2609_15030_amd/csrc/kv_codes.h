@@ -134,25 +134,19 @@ __device__ inline uint32_t wave_most(uint32_t m) {
 // its own without a sum over the sequences before it: n tokens lie in at most n / bt + 2
 // blocks.
 __device__ inline bool spot_of(const KvWriteArgs &a, int64_t w, int *seq, int *c0, int *c1, int *len, int64_t *nth) {
-    const int lane = threadIdx.x & 63;
-    // no sequence before (w - n_tokens / bt) / 2 has this number
-    const int64_t least = (w - (a.n_tokens >> a.bt_shift)) / 2 - 1;
-    for (int i0 = (int)max((int64_t)0, least) & ~63; i0 < a.n_seqs; i0 += 64) {
-        const int i = min(i0 + lane, a.n_seqs - 1);
-        const int n = a.kv_len[i];                 // beside the offsets, not after the sequence is known
-        const int64_t b0 = max(a.cu[i], 0), b1 = min((int64_t)max(a.cu[i + 1], 0), a.n_tokens);
-        const int64_t first = (b0 >> a.bt_shift) + 2 * (int64_t)i, end = (b1 >> a.bt_shift) + 2 * (int64_t)(i + 1);
-        const uint64_t past = __ballot(end > w);
-        if (!past) continue;
-        const int l = __builtin_ctzll(past);
-        *seq = i0 + l;
-        *c0 = __builtin_amdgcn_readlane((int)b0, l);
-        *c1 = __builtin_amdgcn_readlane((int)b1, l);
-        *len = __builtin_amdgcn_readlane(n, l);
-        *nth = w - (((int64_t)__builtin_amdgcn_readlane((int)(first >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)first, l));
-        return *nth >= 0 && *c1 > *c0;
-    }
-    return false;
+    auto first_of = [&](int i) { return (int64_t)(max(a.cu[i], 0) >> a.bt_shift) + 2 * (int64_t)i; };
+    const int i0 = narrow_to_64(a.n_seqs, [&](int i) { return first_of(i + 1) > w; });
+    const int i = min(i0 + (int)(threadIdx.x & 63), a.n_seqs - 1);
+    const int b0 = max(a.cu[i], 0), b1 = max(a.cu[i + 1], 0), n = a.kv_len[i];       // lengths beside the offsets
+    const uint64_t past = __ballot((b1 >> a.bt_shift) + 2 * (int64_t)(i + 1) > w);
+    if (!past) return false;
+    const int l = __builtin_ctzll(past);
+    *seq = i0 + l;
+    *c0 = __builtin_amdgcn_readlane(b0, l);
+    *c1 = __builtin_amdgcn_readlane(b1, l);
+    *len = __builtin_amdgcn_readlane(n, l);
+    *nth = w - (*c0 >> a.bt_shift) - 2 * (int64_t)*seq;
+    return *nth >= 0 && *c1 > *c0;
 }
 
 struct KvCodesArgs {
@@ -182,8 +176,10 @@ __global__ __launch_bounds__(256) void kv_write_codes_kernel(KvCodesArgs args) {
         return;
     }
     // rows [a0, a1) of the block are written, those before a0 stay
-    const int bt = 1 << a.bt_shift, a0 = (int)max(p0 - base, (int64_t)0), a1 = (int)min(len - base, (int64_t)bt);
     const int64_t tok0 = c0 + (base - p0);                     // token of row 0
+    const int bt = 1 << a.bt_shift, a0 = (int)max(p0 - base, (int64_t)0);
+    const int a1 = (int)min(min(len - base, (int64_t)bt), a.n_tokens - tok0);
+    if (a1 <= a0) return;                                      // offsets past the call's rows
     const int team = 1 << args.team_shift, tw = wave & (team - 1), unit = (ug << (2 - args.team_shift)) + (wave >> args.team_shift);
     const bool live = unit < 2 * a.kv_heads;
     const int h = live ? unit >> 1 : 0;
@@ -271,8 +267,7 @@ struct KvReadArgs {
 
 // A wave takes as many tokens as fill it, four 16-byte pieces of the result a lane: with
 // one token a wave, few or short heads left most lanes without work (8 heads of 64: 1.3
-// times the time that a copy takes).  Sequences are found once, for the wave's first
-// token; a lane goes on from there to its own.
+// times the time that a copy takes).
 template <typename T, typename C, int D>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs args) {
     const KvWriteArgs &a = args.w;
@@ -281,22 +276,31 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs args) {
     const int group = args.by_lanes(lane), per_wave = args.by_lanes(64);
     const int64_t first = a.first_token + ((int64_t)blockIdx.x * kWriteTokens + wave) * per_wave, tok = first + group;
     if (first >= a.n_tokens) return;
-    int seq = -1, end = 0;
-    for (int i0 = 0; i0 < a.n_seqs && seq < 0; i0 += 64) {
-        const int c1 = a.cu[min(i0 + lane, a.n_seqs - 1) + 1];
-        const uint64_t past = __ballot(c1 > first);
-        if (!past) continue;
-        const int at = __builtin_ctzll(past);
-        seq = i0 + at;
-        end = __builtin_amdgcn_readlane(c1, at);
+    // the wave's first token's sequence, then those of the others, in the same 64 or behind them
+    const bool mine = group < per_wave && tok < a.n_tokens;
+    int i0 = narrow_to_64(a.n_seqs, [&](int i) { return a.cu[i + 1] > first; });
+    int i = min(i0 + lane, a.n_seqs - 1), c0 = a.cu[i], c1 = a.cu[i + 1], len = a.kv_len[i], seq = -1, pos = 0;
+    bool in = false;
+    for (uint64_t left = __ballot(mine); left;) {
+        const int t = __builtin_amdgcn_readlane((int)tok, __builtin_ctzll(left));
+        const uint64_t past = __ballot(c1 > t);
+        if (!past) {
+            if ((i0 += 64) >= a.n_seqs) break;
+            i = min(i0 + lane, a.n_seqs - 1);
+            c0 = a.cu[i];
+            c1 = a.cu[i + 1];
+            len = a.kv_len[i];
+            continue;
+        }
+        const int at = __builtin_ctzll(past), end = __builtin_amdgcn_readlane(c1, at);
+        if (mine && seq < 0 && (int)tok < end) {
+            seq = i0 + at;
+            pos = __builtin_amdgcn_readlane(len, at) - (end - (int)tok);
+            in = (int)tok >= __builtin_amdgcn_readlane(c0, at);
+        }
+        left = __ballot(mine && seq < 0);
     }
-    if (seq < 0) return;
-    while (tok >= end) {
-        if (++seq >= a.n_seqs) return;
-        end = a.cu[seq + 1];
-    }
-    if (group >= per_wave || tok >= a.n_tokens || tok < a.cu[0]) return;
-    const int pos = a.kv_len[seq] - (end - (int)tok);
+    if (!in) return;
     const int64_t j = pos >> a.bt_shift;
     int id = pos >= 0 && j < a.max_blocks ? a.table[seq * a.max_blocks + j] : -1;
     const bool named = (uint32_t)id < (uint32_t)a.n_blocks;

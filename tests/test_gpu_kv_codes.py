@@ -208,6 +208,52 @@ def test_another_stream_and_a_captured_write():
         c.same(f"replay {step}")
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_many_short_and_empty_sequences(kind):
+    """1,200 of them, most of them empty, the others of 1 to 3 tokens: written, and read back by rows of 8 and of 64 lanes."""
+    gen = torch.Generator().manual_seed(29)
+    new = torch.randint(-4, 4, (1200,), generator=gen).clamp(min=0).tolist()
+    kv = [n + int(x) for n, x in zip(new, torch.randint(0, 20, (1200,), generator=gen))]
+    for H, d in ((1, 64), (5, 128)):
+        table, blocks = tables(gen, kv, 16)
+        c = CodeCache(gen, kind, H, d, 16, table, blocks, layers=1, filled=False)
+        k, v = _rows(gen, sum(new), H, d)
+        cu = _offsets_fast(new)
+        la.la_kv_write(c.layer(), k, v, cu, _i32(kv))
+        c.write(k, v, cu.tolist(), kv)
+        yk, yv = torch.empty_like(k, dtype=torch.float32), torch.empty_like(v, dtype=torch.float32)
+        la.la_kv_read(c.layer(), yk, yv, cu, _i32(kv))
+        torch.cuda.synchronize()
+        c.same(kind)
+        assert int(c.err) == 0
+        for half, y in ((0, yk), (1, yv)):
+            code, scale = c.numbers(half)
+            seq = np.repeat(np.arange(1200), new)
+            pos = np.concatenate([np.arange(L - n, L) for n, L in zip(new, kv)])
+            block = table[seq, pos // 16]
+            assert np.array_equal(y.double().cpu().numpy(), code[block, :, pos % 16] * scale[block][..., None])
+
+
+def _offsets_fast(new):
+    return torch.cumsum(torch.tensor([0] + new), 0).to(torch.int32).cuda()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_offsets_past_the_rows(kind):
+    """Tokens that cu_seqlens has and the call's rows have not are not written; the others are where they belong."""
+    gen = torch.Generator().manual_seed(30)
+    table, blocks = tables(gen, [70, 50], 16)
+    c = CodeCache(gen, kind, 2, 64, 16, table, blocks)
+    k, v = _rows(gen, 40, 2, 64)
+    la.la_kv_write(c.layer(), k[:30].contiguous(), v[:30].contiguous(), _i32([0, 20, 40]), _i32([65, 50]))
+    c.write(k, v, [0, 20], [65])
+    keep, c.table = c.table, c.table[1:]
+    c.write(k, v, [20, 30], [40])                                # the second's first ten: keys 30 to 39
+    c.table = keep
+    torch.cuda.synchronize()
+    c.same(kind)
+
+
 # --- reads -----------------------------------------------------------------------
 
 READS = [([1], [1], 1, 64, 16), ([5, 0, 40, 16], [21, 9, 57, 16], 2, 128, 16), ([100, 33], [131, 33], 3, 64, 32),

@@ -116,6 +116,22 @@ def test_positions_from_the_lengths():
         assert (y[:first] == 3.0).all() and (y[rows.stop:] == 3.0).all()
 
 
+def test_thousands_of_sequences():
+    gen = torch.Generator().manual_seed(59)
+    new = torch.randint(-4, 4, (5000,), generator=gen).clamp(min=0)
+    kv = new + torch.randint(0, 2000, (5000,), generator=gen)
+    T = int(new.sum())
+    cu = torch.cumsum(torch.cat([torch.zeros(1, dtype=torch.int64), new]), 0)
+    pos = torch.cat([torch.arange(int(L - n), int(L)) for n, L in zip(new, kv)])
+    x = _make(gen, T, 1, 64, "bf16", False)
+    rope, y, z = api.Rope(64), torch.empty_like(x), torch.empty_like(x)
+    rope.apply(x, None, y, cu_seqlens=cu.to(torch.int32).cuda(), kv_len=kv.to(torch.int32).cuda())
+    rope.apply(x, None, z, positions=pos.to(torch.int32).cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(y, z)
+    _check(z[-300:], x[-300:], pos[-300:].tolist(), rope, "bf16")
+
+
 @pytest.mark.parametrize("scaling", [("linear", 4.0), ("base", 8.0), ("parts", 8.0, 4096.0, 1.0, 32.0)], ids=lambda s: s[0])
 def test_far_positions_under_a_scaling(scaling):
     """Up to the ends of an int32, where an angle in fp32 would be none."""
@@ -230,3 +246,5 @@ def test_the_binding_refuses(bad):
         k = k[:3]
     with pytest.raises(ValueError):
         rope.apply(q, k, **kw)
+    with pytest.raises(ValueError):
+        rope.apply(None, None, positions=_i32([]))
