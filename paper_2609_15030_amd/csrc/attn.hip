@@ -263,8 +263,9 @@ la_status check_qo(const la_attn_shape *s, const void *q, const void *o, la::Att
 // --- decode ------------------------------------------------------------------
 
 // Workgroups for own keys: two on every CU.  Those of shared prefixes come on top and
-// start first; the own keys' follow as they end.
-constexpr int kRowsGrid = 512;
+// start first; the own keys' follow as they end.  Three on every CU where a cache in one
+// byte a value is read and nothing is shared.
+constexpr int kRowsGrid = 512, kOwnRowsGrid = 768;
 
 struct DecodePlan {
     int own_parts, prefix_parts;
@@ -288,8 +289,14 @@ la_status check_decode_sizes(const la_attn_shape *s, int64_t max_kv_len, int64_t
 
 template <typename T, typename C, int D>
 la_status launch_decode(const la::AttnArgs &a, int64_t rows_blocks, hipStream_t st) {
-    hipLaunchKernelGGL((la::attn_decode_kernel<T, C, D>), dim3((unsigned)(a.prefix_items + rows_blocks)), dim3(la::kRowsThreads), 0,
-                       st, a);
+    bool own = false;
+    if constexpr (sizeof(C) == 1) {
+        own = a.prefix_items == 0;
+        if (own) hipLaunchKernelGGL((la::attn_decode_own_kernel<T, C, D>), dim3((unsigned)rows_blocks), dim3(la::kRowsThreads), 0, st, a);
+    }
+    if (!own)
+        hipLaunchKernelGGL((la::attn_decode_kernel<T, C, D>), dim3((unsigned)(a.prefix_items + rows_blocks)), dim3(la::kRowsThreads), 0,
+                           st, a);
     if (la_status e = hip_check("attention decode launch")) return e;
     if (a.direct) return LA_OK;
     hipLaunchKernelGGL((la::attn_join_kernel<T, D>), dim3((unsigned)(a.n_seqs * a.kv_heads * a.group)), dim3(256), 0, st, a);
@@ -550,7 +557,8 @@ la_status la_attn_decode(const la_attn_shape *shape, const la_kv_layer *layer, c
     if (items > kMaxInt || rows > max_grid(256) || prefix_items + kRowsGrid > max_grid(la::kRowsThreads))
         return fail(LA_ERR_INVALID_ARG, "too many parts for one launch");
     a.prefix_items = (int32_t)prefix_items;
-    const int64_t blocks = std::min<int64_t>(items, kRowsGrid);
+    const bool wide_cache = layer->dtype == LA_F32 || layer->dtype == LA_BF16;
+    const int64_t blocks = std::min<int64_t>(items, wide_cache || prefix_items ? kRowsGrid : kOwnRowsGrid);
     hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
     if (layer->dtype == LA_F32) return decode_of_dim<float, float>(shape->head_dim, a, blocks, st);

@@ -10,10 +10,10 @@
 // end.
 //
 // Many long sequences are bound by memory: 96 of 1 to 32,768 keys, 4 key heads of
-// 128 in 8 bits, 66 us at 4.8 TB/s (a large copy reaches 5.1), their join 5.6; whole
-// calls of 64 of 8,000 in bf16 207 us at 5.1, in 8 bits 131 at 4.0, of 64 of 4,000 with
-// 8 key heads in fp32 378 at 5.5.  A scale for each block and head takes 0.7 % (e4m3) or
-// 2.5 % (int8) of such a call.  A single one is a chain (lengths -> table -> keys ->
+// 128 in 8 bits, 64 us at 5.0 TB/s (a large copy reaches 5.1), their join 5.6; whole
+// calls of 64 of 8,000 in bf16 207 us at 5.1, in 8 bits 128 at 4.1, of 64 of 4,000 with
+// 8 key heads in fp32 378 at 5.5.  A scale for each block and head takes 0.9 % (e4m3) or
+// 1.9 % (int8) of such a call.  A single one is a chain (lengths -> table -> keys ->
 // join): 3,584 keys, 2 heads, 7.5 us, its join 2.6.  64 sequences behind 6,144 shared keys: 22.9 us, of which
 // memory alone would take 9.5; a prefix part is a chain of four key tiles.
 #pragma once
@@ -348,6 +348,18 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_decode_kernel(AttnArgs a
     } else {
         rows_run<T, C, D>(a, (int)blockIdx.x - a.prefix_items, (int)gridDim.x - a.prefix_items, sm.rows);
     }
+}
+
+// Own keys alone, of a cache in one byte a value: without the prefixes' tiles beside them
+// three workgroups share a CU, and 768 of them take 96 sequences of 1 to 32,768 keys in
+// 81.6 us a call (int8; e4m3 80.8) where 512 of the kernel above take 83.9 (82.8) and
+// 1,024, a quarter of which start late, 92.3; 64 of 1,000 20.8 against 22.3, 256 of 4,000
+// with 8 key heads of 64 239 against 258.  Nothing that was timed got slower.  Caches of wider values would spill.
+template <typename T, typename C, int D>
+__global__ __launch_bounds__(kRowsThreads, 3) void attn_decode_own_kernel(AttnArgs a) {
+    static_assert(sizeof(C) == 1, "registers for three workgroups a CU");
+    __shared__ RowsLds<T, D> sm;
+    rows_run<T, C, D>(a, (int)blockIdx.x, (int)gridDim.x, sm);
 }
 
 // Joins the parts of prompt rows, those of the sequences that have several: D / 4

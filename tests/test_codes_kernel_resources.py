@@ -23,6 +23,7 @@ def test_nothing_spills_to_memory(kernels):                  # noqa: F811
 
 @pytest.mark.parametrize("pattern,least", [
     (r"attn_(wide|decode)_kernel.*_code", 2),
+    (r"attn_decode_own_kernel", 3),                          # a grid of three a CU
     (r"kv_write_codes_kernel", 4),                           # 16 waves with 16 KB each in flight
     (r"kv_read_kernel", 7),
     (r"rope_kernel", 6),
