@@ -31,6 +31,16 @@ def e4m3(x):
     return np.where(np.isnan(x), np.nan, np.copysign(E4M3[pick], x))
 
 
+def bf16(x):
+    """Nearest bf16 numbers of fp64 values, ties to the even one."""
+    x = np.asarray(x, np.float64)
+    finite = np.isfinite(x)
+    unit = np.ldexp(1.0, np.maximum(np.frexp(np.where(finite, x, 0.0))[1] - 8, -133))       # of the last of 8 significant bits
+    y = np.rint(np.where(finite, x, 0.0) / unit) * unit
+    y = np.where(np.abs(y) >= 2.0 ** 128, np.copysign(np.inf, y), y)
+    return np.where(finite, y, x)
+
+
 def codes(x, kind):
     return e4m3(x) if kind == "e4m3" else np.rint(np.where(np.isnan(x), 0.0, x))
 
