@@ -67,7 +67,7 @@ def scale_of(most: float, kind: str) -> float:
 def held(s: float, kind: str) -> float:
     """A block's scale as a later write sees it: one that no write can have left is the least."""
     s = float(s)
-    if not (float(LEAST) <= s <= 2.0 ** 127):
+    if not (float(LEAST) <= s <= scale_of(LARGEST, kind)):
         return float(LEAST)
     m = Fraction(s)
     while m >= (2 if kind == "e4m3" else 256):

@@ -40,10 +40,12 @@ template <typename C> __device__ inline float scale_of(float most) {
     return fmaxf(s, kLeastScale);
 }
 
-// A scale that a block holds; what no write can have left there counts as the least.
+// A scale that a block holds; what no write can have left there counts as the least.  The
+// largest that one can is that of 2^127: past it (a stray scale in a block that is used
+// again) ordinary tokens would all become code 0.
 template <typename C> __device__ inline float held_scale(float s) {
     const float t = __uint_as_float(__float_as_uint(s) & (kScaleCodes<C> ? 0xFF800000u : 0xFFFF0000u));
-    return s == t && s >= kLeastScale && s <= 0x1p127f ? s : kLeastScale;
+    return s == t && s >= kLeastScale && s <= scale_of<C>(__uint_as_float(kLargestBf16 << 16)) ? s : kLeastScale;
 }
 
 // x / s correctly rounded where the quotient has few bits (a tie), by r = 1 / s: the
