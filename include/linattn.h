@@ -629,7 +629,8 @@ typedef struct la_rope_scaling {
 la_status la_rope_frequencies(int32_t rotary_dim, double base, const la_rope_scaling *scaling, double *freq_out);
 
 /* la_rope_turns - n frequencies (any finite ones) as la_rope_apply reads them:
- * the fraction of a turn that a token adds, in units of 2^-64.  Host only. */
+ * the fraction of a turn that a token adds, in units of 2^-64, off by at most four
+ * of them however many whole turns it adds.  Host only. */
 la_status la_rope_turns(const double *freq, int32_t n, uint64_t *turns_out);
 
 typedef struct la_rope_plan {
@@ -665,7 +666,7 @@ typedef struct la_rope_positions {
  * la_rope_apply - turns the rows of q and of k (either may be NULL) in one
  * launch.  transpose: by the opposite angles, with the same magnitude, which is
  * the gradient: of y's gradient it makes x's.  An angle is off by at most
- * 2e-7 radians at any position.
+ * 2e-7 radians at any position and frequency.
  */
 la_status la_rope_apply(const la_rope_plan *plan, const la_rope_rows *q, const la_rope_rows *k, int64_t n_tokens,
                         const la_rope_positions *at, int32_t transpose, void *stream);

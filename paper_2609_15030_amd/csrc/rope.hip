@@ -84,7 +84,11 @@ la_status la_rope_turns(const double *freq, int32_t n, uint64_t *turns_out) {
     for (int i = 0; i < n; ++i)
         if (!std::isfinite(freq[i])) return fail(LA_ERR_INVALID_ARG, "freq[%d]=%g", i, freq[i]);
     for (int i = 0; i < n; ++i) {
-        const long double t = (long double)freq[i] / 6.283185307179586476925286766559L, x = std::ldexp(t - std::floor(t), 64);
+        // beyond half a turn the quotient would have fewer than 64 bits behind its whole turns: the
+        // angle in (-pi, pi] by its sine and cosine, which the C library reduces exactly
+        long double f = freq[i];
+        if (std::fabs(f) > 3.14L) f = std::atan2(std::sin(f), std::cos(f));
+        const long double t = f / 6.283185307179586476925286766559L, x = std::ldexp(t - std::floor(t), 64);
         turns_out[i] = x < 18446744073709551615.0L ? (uint64_t)x : 0;
     }
     return LA_OK;
