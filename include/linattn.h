@@ -445,8 +445,9 @@ la_status la_state_restore_host(const float *host_pool, int64_t n_pages, const i
  * exception: an infinite value with a weight that rounds to zero gives
  * infinity or NaN).  Values are summed before the division: beyond 2^120 / keys
  * the sums may overflow.  Scores, maxima and sums are fp32 (a token with a score past
- * fp32's range has NaN); with bf16 inputs the
- * weights p_j are rounded to bf16 for the product with v (times the value scale, where
+ * fp32's range has NaN; over int8 codes, whose scales come after the product, also
+ * where the sum of q times codes, or scale times a block's scale, passes it); with
+ * bf16 inputs the weights p_j are rounded to bf16 for the product with v (times the value scale, where
  * int8 codes have one for each block).  Keys and values of an 8-bit cache are what its
  * codes stand for: k_scale or the block's scale times the code.  The same call
  * gives the same bits.  A single token's result does not depend on the other

@@ -221,8 +221,10 @@ struct Runs {
 };
 
 // What the scores of a run with key scale ks are multiplied by.  Not zero: masked scores
-// are minus infinity when they are multiplied.
-__device__ inline float run_factor(float c, float ks) { return fmaxf(c * ks, 0x1p-126f); }
+// are minus infinity when they are multiplied.  The least subnormal: a factor is off by at
+// most 2^-149 then, and a score of fp32's size by 2^-21, where the least normal number would
+// let large queries give keys of the least scale up to 16 times their weight.
+__device__ inline float run_factor(float c, float ks) { return fmaxf(c * ks, 0x1p-149f); }
 
 // Maximum and sum over the four lanes (l, l + 16, l + 32, l + 48) that share a
 // q row of a 16-column accumulator.
