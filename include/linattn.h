@@ -559,8 +559,8 @@ size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv
  * are not written, so a part of a batch's sequences serves.  A position
  * below zero or past the table counts in err_count and is not written.
  *
- * LA_FP8_E4M3 holds x / scale rounded to nearest even, values beyond +-448 at
- * +-448, NaN as NaN.
+ * LA_FP8_E4M3 holds x / scale, a quotient in fp32, rounded to nearest even, values
+ * beyond +-448 at +-448, NaN as NaN.
  *
  * LA_FP8_E4M3_BLOCK and LA_INT8_BLOCK hold codes x / s rounded to nearest even,
  * with a scale s for the keys and one for the values of each block and head,
@@ -571,7 +571,7 @@ size_t la_attn_decode_workspace_bytes(const la_attn_shape *shape, int64_t max_kv
  * and at least 2^-100.  Where tokens before the call's stay in the block, s is
  * no less than the block's scale, and if it is greater their codes become
  * code * old / s, rounded to nearest even; a block's scale that no write can
- * have left counts as 2^-100.  Values beyond +-2^127 (infinities too) are
+ * have left (past that of values of 2^127, or of more bits) counts as 2^-100.  Values beyond +-2^127 (infinities too) are
  * written as +-2^127.  NaN: e4m3 holds it; int8, which cannot, holds 0 and
  * counts in err_count.  No call may write into one block through two entries
  * of its tables.

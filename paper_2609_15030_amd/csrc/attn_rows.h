@@ -10,12 +10,12 @@
 // end.
 //
 // Many long sequences are bound by memory: 96 of 1 to 32,768 keys, 4 key heads of
-// 128 in 8 bits, 64 us at 5.0 TB/s (a large copy reaches 5.1), their join 5.6; whole
-// calls of 64 of 8,000 in bf16 207 us at 5.1, in 8 bits 128 at 4.1, of 64 of 4,000 with
-// 8 key heads in fp32 378 at 5.5.  A scale for each block and head takes 0.9 % (e4m3) or
-// 1.9 % (int8) of such a call.  A single one is a chain (lengths -> table -> keys ->
+// 128, 128 us in bf16 (5.0 TB/s of keys and values, what a large copy reaches), 72 in 8 bits
+// (4.4; 73 and 74 over e4m3 and int8 with a scale for each block and head), their join 5.4;
+// whole calls of 64 of 8,000 in bf16 207 us at 5.1, in 8 bits 126 at 4.2, of 64 of 4,000 with
+// 8 key heads in fp32 377 at 5.5.  A single one is a chain (lengths -> table -> keys ->
 // join): 3,584 keys, 2 heads, 7.5 us, its join 2.6.  64 sequences behind 6,144 shared keys: 22.9 us, of which
-// memory alone would take 9.5; a prefix part is a chain of four key tiles.
+// memory alone would take 9.5 (8 bits 17.3, 4.8); a prefix part is a chain of four key tiles.
 #pragma once
 #include "attn_tile.h"
 #include "attn_wide.h"

@@ -6,10 +6,10 @@
 // 32,768 tokens; 64 rows a wave leave one wave a SIMD, whose own exponentials
 // then wait for its products: 860).  As it stands the kernel takes that prompt at
 // 1,025 to 1,048 TFLOP/s, from card to card (a product of 8,192 x 8,192 x 8,192:
-// 1,177 to 1,200), the suffixes of 16 prompts over an 8-bit cache at 893 to 923, over one
-// with a scale for each block and head at 918 (e4m3) and 825 (int8, whose conversion to
-// bf16 takes three times the instructions) where the plain one has 928, and over a bf16
-// one at 882 to 896.
+// 1,177 to 1,200), the suffixes of 16 prompts over an 8-bit cache at 893 to 936, over one
+// with a scale for each block and head at 876 to 926 (e4m3; 1 % below the plain one on the
+// same card) and 825 to 831 (int8, whose conversion to bf16 takes three times the
+// instructions), and over a bf16 one at 882 to 899.
 //
 // A row's chain is scores -> maximum -> weights -> product with V.  A wave runs it
 // as a pipeline of half tiles (32 keys): while the weights of half h are formed,
